@@ -189,7 +189,8 @@ def _own(c):
         elif op == "prompt":
             c["ws"] = tcuscan.new_decay_attention_workspace(c["rows"], c["total"], c["heads"], c["dk"], c["dv"])
         else:
-            c["ws"] = tcuscan.new_decay_attention_backward_workspace(c["rows"], c["total"], c["heads"], c["dk"], c["dv"])
+            c["ws"] = tcuscan.new_decay_attention_backward_workspace(c["rows"], c["total"], c["heads"], c["dk"], c["dv"],
+                                                                     c["q_heads"], c["k_heads"], c["v_heads"])
     if op == "lookup_grad":
         tcuscan.embedding_backward(c["ids"], c["d_out"], c["d_weight"], scale=c["scale"], ws=c["ws"])
         return [c["d_weight"]]
