@@ -351,6 +351,96 @@ tcuscan_status_t tcuscan_split_radix_sort_u32(void *d_keys, void *d_vals, size_t
  * is the same. */
 tcuscan_status_t tcuscan_set_sort_fusion(int fused);
 
+/*
+ * Linear attention with one decay per head: the prefix sum whose elements are matrices and whose sums decay.  Row by row and head
+ * by head, with a_h = exp(d_log_decay[h]) and query, key and value of token t as row vectors:
+ *
+ *     S_t = a_h S_(t-1) + k_t^T v_t,    o_t = scale q_t S_t        (S: dk x dv, S before the first token = d_state_in)
+ *
+ * computed for a block of tokens at a time as products with decayed triangular matrices, the state carried from block to block
+ * (Section 2.2's segments and carries).  Rows of tokens lie back to back, as in tcuscan_segmented.
+ *
+ *   shape      sizes and strides, read on the host during the call.  Token t's stored head s of q lies at d_q + t * q_token +
+ *              s * q_head (elements; features are dense); k, v, o and, for the gradients, dq, dk, dv likewise.  Strides may be
+ *              0 or negative for inputs; outputs of different tokens and heads must not overlap each other, nor any input.
+ *              q_heads, k_heads and v_heads divide `heads`: head h takes the stored head h * q_heads / heads, so that shared
+ *              heads need no copies.  dk and dv: 1 to 256.
+ *   d_log_decay  heads fp32 values: log a_h.  0 (no decay) and minus infinity (a = 0) are allowed, positive ones grow.  The decays are
+ *              constants of the model: no gradient by them is computed.
+ *   d_offsets  rows + 1 signed 64-bit token offsets on the DEVICE, non-decreasing, within [0, total].  Rows may be empty.  Tokens in
+ *              front of the first and behind the last offset are neither read nor written.
+ *   dt         the element type of q, k, v, o and their gradients, named by the dtype whose INPUT it is: TCUSCAN_F16_F32,
+ *              TCUSCAN_BF16_F32 or TCUSCAN_F32_F32.  States, decays and all sums are fp32.
+ *   d_state_in, d_state_out   [states][heads][dk][dv] fp32, 16-byte aligned, or NULL: rows start from zeros / the states behind the
+ *              rows are not wanted.  Both may be the same array.
+ *   d_slots    NULL: row r has state r (states >= rows).  Otherwise rows signed 64-bit DEVICE values: row r has state d_slots[r];
+ *              a negative one means none (the row starts from zeros, what it ends in is dropped).  Rows that share a state race.
+ *   d_ws       tcuscan_decay_attention_workspace_bytes(shape, dt, 0) bytes (its `backward` argument 1 for the gradients'), 16-byte
+ *              aligned, zero-filled once.  An offset or slot out of range sets its fault word to 2
+ *              (tcuscan_workspace_fault); nothing outside the arrays is touched then, and the results are unspecified.
+ *
+ * Inputs must be finite.  A value that is not spoils outputs of its own row and heads, also up to 63 tokens in front of it, and none
+ * of other rows.  16-bit outputs are rounded once from fp32 sums; what the products round on the way is at most as much again.
+ */
+typedef struct {
+    long long rows, total, heads, dk, dv;
+    long long q_heads, k_heads, v_heads;
+    long long q_token, q_head, k_token, k_head, v_token, v_head, o_token, o_head;
+    long long dq_token, dq_head, dk_token, dk_head, dv_token, dv_head; /* gradients only */
+} tcuscan_attention_shape_t;
+
+size_t tcuscan_decay_attention_workspace_bytes(const tcuscan_attention_shape_t *shape, tcuscan_dtype_t dt, int backward);
+tcuscan_status_t tcuscan_decay_attention(const tcuscan_attention_shape_t *shape, const void *d_q, const void *d_k, const void *d_v, void *d_o,
+                                         const float *d_log_decay, const long long *d_offsets, tcuscan_dtype_t dt, float scale,
+                                         const float *d_state_in, float *d_state_out, const long long *d_slots, size_t states,
+                                         void *d_ws, size_t ws_bytes, tcuscan_stream_t stream);
+
+/*
+ * Its gradients.  d_o_grad (strides o_token, o_head) and d_state_out_grad ([rows][heads][dk][dv] fp32 or NULL: zeros) are the gradients
+ * by o and by the states behind the rows; d_state_in is what the rows started from (or NULL).  Writes the gradients by q, k and v
+ * (stored heads that several heads share: summed over these in fp32, in the order of the heads) and, if not NULL, by d_state_in.
+ */
+tcuscan_status_t tcuscan_decay_attention_backward(const tcuscan_attention_shape_t *shape, const void *d_q, const void *d_k, const void *d_v,
+                                                  const void *d_o_grad, void *d_q_grad, void *d_k_grad, void *d_v_grad,
+                                                  const float *d_log_decay, const long long *d_offsets, tcuscan_dtype_t dt, float scale,
+                                                  const float *d_state_in, const float *d_state_out_grad, float *d_state_in_grad,
+                                                  void *d_ws, size_t ws_bytes, tcuscan_stream_t stream);
+
+/*
+ * One token for each of `rows` sequences (shape->total == shape->rows): token i's state is d_state[d_slots[i]] (NULL: d_state[i]), of
+ * `states` in all, and is updated in place.  A negative slot: no state, o = scale q (k^T v).  Two tokens with the same slot race.
+ * d_ws: NULL, or a workspace of at least 256 bytes whose fault word is set to 2 where a slot is not below `states`.
+ */
+tcuscan_status_t tcuscan_decay_attention_step(const tcuscan_attention_shape_t *shape, const void *d_q, const void *d_k, const void *d_v, void *d_o,
+                                              const float *d_log_decay, tcuscan_dtype_t dt, float scale, float *d_state,
+                                              const long long *d_slots, size_t states, void *d_ws, size_t ws_bytes, tcuscan_stream_t stream);
+
+/*
+ * Rows of an embedding table: d_out[t] = scale * d_weight[d_ids[t]] for n tokens, computed in fp32 and rounded to the output's type.
+ *   d_ids      n signed token numbers of id_bytes (4 or 8) bytes.  Negative: no token, zeros are written.
+ *   d_weight   vocab rows of dim elements, weight_stride (>= dim) elements apart; d_out likewise.  Types as above, any pair of them.
+ *   d_ws       NULL, or a workspace of at least 256 bytes: its fault word is set to 2 where a number is not below vocab (zeros are
+ *              written there, too)
+ */
+tcuscan_status_t tcuscan_embedding(const void *d_ids, int id_bytes, size_t n, const void *d_weight, size_t vocab, size_t dim,
+                                   size_t weight_stride, tcuscan_dtype_t weight_dt, void *d_out, size_t out_stride, tcuscan_dtype_t out_dt,
+                                   float scale, void *d_ws, size_t ws_bytes, tcuscan_stream_t stream);
+
+/*
+ * Its gradient by the table: d_weight_grad[r] = scale * (the sum of d_out_grad[t] over the tokens t with d_ids[t] == r), the sums in
+ * fp32 and in an order that the sorted tokens alone fix (the same bits on every run).  Every row is written, zeros where no token is; with
+ * TCUSCAN_ACCUMULATE the sums are added to what is there, and rows without a token are not touched.  Tokens whose number is
+ * negative, not below vocab (fault word 2) or equal to `padding` (-1: none) add nothing.  The tokens are sorted by their numbers with
+ * tcuscan_split_radix_sort_u32.  n < 2^32.
+ *   d_ws       tcuscan_embedding_backward_workspace_bytes(n, vocab, dim) bytes, 16-byte aligned, zero-filled once
+ */
+#define TCUSCAN_ACCUMULATE 1u
+size_t tcuscan_embedding_backward_workspace_bytes(size_t n, size_t vocab, size_t dim);
+tcuscan_status_t tcuscan_embedding_backward(const void *d_ids, int id_bytes, size_t n, const void *d_out_grad, size_t out_stride,
+                                            tcuscan_dtype_t out_dt, void *d_weight_grad, size_t vocab, size_t dim, size_t weight_stride,
+                                            tcuscan_dtype_t weight_dt, float scale, long long padding, unsigned flags,
+                                            void *d_ws, size_t ws_bytes, tcuscan_stream_t stream);
+
 /* Static, human-readable name of a status code. */
 const char *tcuscan_status_string(tcuscan_status_t st);
 

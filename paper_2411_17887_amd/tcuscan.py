@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libtcuscan.so")
@@ -22,7 +23,9 @@ EXPORTS = ["tcuscan_workspace_bytes", "tcuscan_workspace_init", "tcuscan_inclusi
            "tcuscan_workspace_fault", "tcuscan_matmulscan_levels", "tcuscan_matmulscan_levels_radix", "tcuscan_compact_u32",
            "tcuscan_split_radix_sort_u32", "tcuscan_set_sort_fusion", "tcuscan_status_string",
            "tcuscan_set_chain_policy", "tcuscan_scan_static", "tcuscan_path_for", "tcuscan_measure_stream",
-           "tcuscan_test_advance_calls", "tcuscan_test_tag_period", "tcuscan_test_chain_fault"]
+           "tcuscan_test_advance_calls", "tcuscan_test_tag_period", "tcuscan_test_chain_fault",
+           "tcuscan_decay_attention_workspace_bytes", "tcuscan_decay_attention", "tcuscan_decay_attention_backward",
+           "tcuscan_decay_attention_step", "tcuscan_embedding", "tcuscan_embedding_backward_workspace_bytes", "tcuscan_embedding_backward"]
 
 _lib = None
 
@@ -88,7 +91,18 @@ def load() -> ctypes.CDLL:
         L.tcuscan_test_chain_fault.restype = ci
         L.tcuscan_status_string.argtypes = [ci]
         L.tcuscan_status_string.restype = ctypes.c_char_p
-        for f in ("tcuscan_workspace_init", "tcuscan_inclusive", "tcuscan_exclusive", "tcuscan_batched", "tcuscan_scan", "tcuscan_segmented",
+        cf, ll = ctypes.c_float, ctypes.c_longlong
+        L.tcuscan_decay_attention_workspace_bytes.argtypes = [vp, ci, ci]
+        L.tcuscan_decay_attention_workspace_bytes.restype = sz
+        L.tcuscan_decay_attention.argtypes = [vp] * 7 + [ci, cf, vp, vp, vp, sz, vp, sz, vp]
+        L.tcuscan_decay_attention_backward.argtypes = [vp] * 10 + [ci, cf, vp, vp, vp, vp, sz, vp]
+        L.tcuscan_decay_attention_step.argtypes = [vp] * 6 + [ci, cf, vp, vp, sz, vp, sz, vp]
+        L.tcuscan_embedding.argtypes = [vp, ci, sz, vp, sz, sz, sz, ci, vp, sz, ci, cf, vp, sz, vp]
+        L.tcuscan_embedding_backward_workspace_bytes.argtypes = [sz, sz, sz]
+        L.tcuscan_embedding_backward_workspace_bytes.restype = sz
+        L.tcuscan_embedding_backward.argtypes = [vp, ci, sz, vp, sz, ci, vp, sz, sz, sz, ci, cf, ll, ctypes.c_uint, vp, sz, vp]
+        for f in ("tcuscan_decay_attention", "tcuscan_decay_attention_backward", "tcuscan_decay_attention_step", "tcuscan_embedding",
+                  "tcuscan_embedding_backward", "tcuscan_workspace_init", "tcuscan_inclusive", "tcuscan_exclusive", "tcuscan_batched", "tcuscan_scan", "tcuscan_segmented",
                   "tcuscan_workspace_fault", "tcuscan_matmulscan_levels", "tcuscan_matmulscan_levels_radix",
                   "tcuscan_compact_u32", "tcuscan_split_radix_sort_u32"):
             getattr(L, f).restype = ci
@@ -301,3 +315,172 @@ def workspace_fault(ws, stream=None) -> int:
     if rc != OK:
         raise TcuscanError(rc, "tcuscan_workspace_fault")
     return int(v.value)
+
+
+# ---- operators on tokens: linear attention with decays, embeddings
+
+ACCUMULATE = 1                 # flag bit of tcuscan_embedding_backward
+_ELEMENTS = {}                 # torch.dtype -> the dtype whose input it is
+_pack_shape = struct.Struct("22q").pack
+
+
+def _element(t) -> int:
+    if not _ELEMENTS:
+        import torch
+        _ELEMENTS.update({torch.float16: F16_F32, torch.bfloat16: BF16_F32, torch.float32: F32_F32})
+    return _ELEMENTS.get(t.dtype, -1)
+
+
+def _refuse(condition, what: str) -> None:
+    if condition:
+        raise ValueError(what)
+
+
+def _attention_shape(rows, q, k, v, out, log_decay, dq=None, dk=None, dv=None) -> tuple[bytes, int]:
+    """The C call's shape and element type, from tensors [token, stored head, feature]."""
+    (total, q_heads, d_k), (k_total, k_heads, k_dim), (v_total, v_heads, d_v), (o_total, heads, o_dim) = q.shape, k.shape, v.shape, out.shape
+    _refuse(not total == k_total == v_total == o_total, "q, k, v and out have different numbers of tokens")
+    _refuse(d_k != k_dim or d_v != o_dim or log_decay.numel() != heads, "features of q and k, of v and out, or heads of out and decays differ")
+    dt = q.dtype
+    _refuse(not dt == k.dtype == v.dtype == out.dtype, "q, k, v and out have different types")
+    (qt, qh, q1), (kt, kh, k1), (vt, vh, v1), (ot, oh, o1) = q.stride(), k.stride(), v.stride(), out.stride()
+    _refuse((q1 != 1 or k1 != 1) and d_k > 1 or (v1 != 1 or o1 != 1) and d_v > 1, "features have to be dense")
+    grads = (0, 0, 0, 0, 0, 0)
+    if dq is not None:
+        for g, x in ((dq, q), (dk, k), (dv, v)):
+            _refuse(g.shape != x.shape or g.dtype != dt or g.stride(2) != 1 and g.shape[2] > 1, "a gradient's shape, type or stride is not its input's")
+        grads = (*dq.stride()[:2], *dk.stride()[:2], *dv.stride()[:2])
+    return _pack_shape(rows, total, heads, d_k, d_v, q_heads, k_heads, v_heads, qt, qh, kt, kh, vt, vh, ot, oh, *grads), _element(q)
+
+
+def _check_states(states, heads: int, d_k: int, d_v: int) -> int:
+    """[states, heads, dk, dv] of fp32, dense.  Returns how many there are."""
+    import torch
+    _refuse(states.dtype != torch.float32 or states.shape[1:] != (heads, d_k, d_v) or not states.is_contiguous(),
+            "states are dense fp32 tensors [states, heads, dk, dv]")
+    return states.shape[0]
+
+
+def _check_longs(t, n: int, what: str) -> None:
+    import torch
+    _refuse(t.dtype != torch.int64 or t.numel() != n or not t.is_contiguous(), f"{what}: a dense int64 tensor of {n} elements is wanted")
+
+
+def _check_decays(t) -> None:
+    import torch
+    _refuse(t.dtype != torch.float32 or not t.is_contiguous(), "log_decay: a dense fp32 tensor is wanted")
+
+
+def _zeros(nbytes: int):
+    import torch
+    return torch.zeros((nbytes + 7) // 8, dtype=torch.int64, device="cuda")
+
+
+def decay_attention_workspace_bytes(rows: int, total: int, heads: int, d_k: int, d_v: int, q_heads=None, k_heads=None, v_heads=None, dt="bf16",
+                                    backward: bool = False) -> int:
+    shape = _pack_shape(rows, total, heads, d_k, d_v, q_heads or heads, k_heads or heads, v_heads or heads, *[0] * 14)
+    return int(load().tcuscan_decay_attention_workspace_bytes(shape, _dt(dt), int(backward)))
+
+
+def new_decay_attention_workspace(rows: int, total: int, heads: int, d_k: int, d_v: int, q_heads=None, k_heads=None, v_heads=None, dt="bf16"):
+    """A zero-filled workspace for decay_attention on up to `rows` rows of `total` tokens in all."""
+    return _zeros(decay_attention_workspace_bytes(rows, total, heads, d_k, d_v, q_heads, k_heads, v_heads, dt))
+
+
+def new_decay_attention_backward_workspace(rows: int, total: int, heads: int, d_k: int, d_v: int, q_heads=None, k_heads=None, v_heads=None,
+                                           dt="bf16"):
+    return _zeros(decay_attention_workspace_bytes(rows, total, heads, d_k, d_v, q_heads, k_heads, v_heads, dt, backward=True))
+
+
+def decay_attention(q, k, v, out, log_decay, offsets, scale: float = 1.0, state_in=None, state_out=None, slots=None, ws=None, stream=None) -> None:
+    """Linear attention with one decay per head over rows of tokens stored back to back.
+
+    q [total, q_heads, dk], k [total, k_heads, dk], v [total, v_heads, dv], out [total, heads, dv]: any strides, features dense;
+    log_decay [heads]; offsets int64 [rows + 1]; state_in, state_out [states, heads, dk, dv] fp32 or None; slots int64 [rows] or None."""
+    rows = offsets.numel() - 1
+    shape, dt = _attention_shape(rows, q, k, v, out, log_decay)
+    _check_decays(log_decay)
+    _check_longs(offsets, rows + 1, "offsets")
+    states = 0
+    for t in (state_in, state_out):
+        if t is not None:
+            n = _check_states(t, out.shape[1], q.shape[2], v.shape[2])
+            _refuse(states and n != states, "state_in and state_out hold different numbers of states")
+            states = n
+    if slots is not None:
+        _check_longs(slots, rows, "slots")
+    rc = load().tcuscan_decay_attention(shape, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), log_decay.data_ptr(), offsets.data_ptr(), dt, scale,
+                                        _ptr(state_in), _ptr(state_out), _ptr(slots), states, *_ws_args(ws), _stream(stream))
+    if rc != OK:
+        raise TcuscanError(rc, "tcuscan_decay_attention")
+
+
+def decay_attention_backward(q, k, v, d_out, dq, dk, dv, log_decay, offsets, scale: float = 1.0, state_in=None, d_state_out=None, d_state_in=None,
+                             ws=None, stream=None) -> None:
+    """The gradients by q, k, v (into dq, dk, dv) and by state_in (into d_state_in, if given) from those by out and by state_out."""
+    rows = offsets.numel() - 1
+    shape, dt = _attention_shape(rows, q, k, v, d_out, log_decay, dq, dk, dv)
+    _check_decays(log_decay)
+    _check_longs(offsets, rows + 1, "offsets")
+    for t in (state_in, d_state_out, d_state_in):
+        if t is not None:
+            _refuse(_check_states(t, d_out.shape[1], q.shape[2], v.shape[2]) != rows, "a state for each row is wanted")
+    rc = load().tcuscan_decay_attention_backward(shape, q.data_ptr(), k.data_ptr(), v.data_ptr(), d_out.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
+                                                 log_decay.data_ptr(), offsets.data_ptr(), dt, scale, _ptr(state_in), _ptr(d_state_out), _ptr(d_state_in),
+                                                 *_ws_args(ws), _stream(stream))
+    if rc != OK:
+        raise TcuscanError(rc, "tcuscan_decay_attention_backward")
+
+
+def decay_attention_step(q, k, v, out, log_decay, state, slots=None, scale: float = 1.0, ws=None, stream=None) -> None:
+    """One token for each of n sequences: q [n, q_heads, dk], ..., out [n, heads, dv]; state [states, heads, dk, dv] fp32, updated in
+    place where slots (int64 [n], None: 0 .. n - 1) point."""
+    n = q.shape[0]
+    shape, dt = _attention_shape(n, q, k, v, out, log_decay)
+    _check_decays(log_decay)
+    states = _check_states(state, out.shape[1], q.shape[2], v.shape[2])
+    if slots is not None:
+        _check_longs(slots, n, "slots")
+    rc = load().tcuscan_decay_attention_step(shape, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), log_decay.data_ptr(), dt, scale, state.data_ptr(),
+                                             _ptr(slots), states, *_ws_args(ws), _stream(stream))
+    if rc != OK:
+        raise TcuscanError(rc, "tcuscan_decay_attention_step")
+
+
+def _check_tokens(ids, rows, table) -> None:
+    """ids: n dense integers of 4 or 8 bytes; rows [n, dim] and table [vocab, dim] with dense features."""
+    _refuse(ids.dtype.is_floating_point or ids.element_size() not in (4, 8) or not ids.is_contiguous(), "ids: a dense tensor of 4- or 8-byte integers is wanted")
+    _refuse(rows.dim() != 2 or table.dim() != 2 or rows.shape[0] != ids.numel() or rows.shape[1] != table.shape[1], "one row of the table's width per token is wanted")
+    _refuse((rows.stride(1) != 1 or table.stride(1) != 1) and table.shape[1] > 1, "features have to be dense")
+
+
+def _row_stride(t) -> int:
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def embedding(ids, weight, out, scale: float = 1.0, ws=None, stream=None) -> None:
+    """out[t] = scale * weight[ids[t]]; zeros where ids[t] is negative (or not below the table's height: fault word 2 of ws)."""
+    _check_tokens(ids, out, weight)
+    rc = load().tcuscan_embedding(ids.data_ptr(), ids.element_size(), ids.numel(), weight.data_ptr(), weight.shape[0], weight.shape[1], _row_stride(weight),
+                                  _element(weight), out.data_ptr(), _row_stride(out), _element(out), scale, *_ws_args(ws), _stream(stream))
+    if rc != OK:
+        raise TcuscanError(rc, "tcuscan_embedding")
+
+
+def embedding_backward_workspace_bytes(n: int, vocab: int, dim: int) -> int:
+    return int(load().tcuscan_embedding_backward_workspace_bytes(n, vocab, dim))
+
+
+def new_embedding_backward_workspace(n: int, vocab: int, dim: int):
+    """A zero-filled workspace for embedding_backward of n tokens."""
+    return _zeros(embedding_backward_workspace_bytes(n, vocab, dim))
+
+
+def embedding_backward(ids, d_out, d_weight, scale: float = 1.0, padding: int = -1, accumulate: bool = False, ws=None, stream=None) -> None:
+    """d_weight[r] = scale * (sum of d_out[t] over the tokens t with ids[t] == r), or added to it; tokens numbered `padding` add nothing."""
+    _check_tokens(ids, d_out, d_weight)
+    rc = load().tcuscan_embedding_backward(ids.data_ptr(), ids.element_size(), ids.numel(), d_out.data_ptr(), _row_stride(d_out), _element(d_out),
+                                           d_weight.data_ptr(), d_weight.shape[0], d_weight.shape[1], _row_stride(d_weight), _element(d_weight), scale,
+                                           int(padding), ACCUMULATE if accumulate else 0, *_ws_args(ws), _stream(stream))
+    if rc != OK:
+        raise TcuscanError(rc, "tcuscan_embedding_backward")
