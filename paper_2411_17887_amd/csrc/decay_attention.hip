@@ -39,13 +39,18 @@ struct WalkArgs {
     const long long *offsets, *slots;              // slots: null, or the state that each row has
     const float *m_in;                             // null: zeros
     float *m_out;                                  // null: not wanted
+    float *between;                                // [piece][head][A][E]: what segments add, then what they start from
     void *ws;
     long long states;                              // how many states there are
     long long total;
     unsigned rows, heads, A, E;
     unsigned m_a, m_e;                             // strides of a state: M[a][e] is at a * m_a + e * m_e
+    unsigned pieces, segment_log2;
     float by_new, by_read;
     int from_end;
+    int wide;                                      // the output is fp32 whatever the element type
+    int whole;                                     // bits 0 to 2: eight elements of x, y, z are aligned 16-byte granules (two for fp32) and
+                                                   // all inside or all outside; bit 3: four elements of the output likewise
 };
 
 // a^n, for weights.  (An n of 0 gives 1 for a decay of 0, a log_decay of minus infinity, too.)
@@ -78,46 +83,408 @@ __device__ __forceinline__ long long state_of(const long long *slots, unsigned r
     return s >= 0 && s < states ? s : -1;
 }
 
-// The walk token by token: a workgroup of one wavefront per (row, head, 64 columns), the state in LDS.
-template <int DT, int DO> __global__ __launch_bounds__(64) void walk_kernel(WalkArgs W)
+// ---------------------------------------------------------------- the walk in blocks of tokens, on the matrix unit
+//
+// C tokens i = 0 .. C-1 of a row (from the end: the last token first) with the state M in front of them:
+//
+//   out_i = by_read (a^(i+1) x_i M + sum over j <= i of by_new a^(i-j) (x_i . y_j) z_j)    (from the end a^i in place of a^(i+1))
+//   M    <- a^C M + sum over j of by_new a^(C-1-j) y_j^T z_j                          (from the end a^(C-j))
+//
+// Every sum over features or tokens is a matrix product: P^T = Y X^T (then weighted and cut to j <= i), out^T = M^T X^T and Z^T P^T,
+// M += Y^T (wZ).  A wavefront owns 16 columns of Z, out and M and all A rows of M, in MFMA accumulators from the first token to the
+// last.  The products are ordered so that operands fall into the lanes that have them: the accumulators of M, two row tiles side by side, are
+// the left operand of M^T X^T as they stand (tile rows are dealt so that a lane's eight values are eight consecutive a), and Z's columns are
+// read transposed once, for Z^T P^T and, weighted, for the update.  Only X, Y, Z (shared by all wavefronts of the workgroup) and P go through LDS.
+//
+// Precision.  The matrix unit multiplies bf16 and adds in fp32, so every operand is a sum of bf16 parts: bf16 inputs one, f16 two (exact),
+// fp32 three.  What is rounded on the way:
+//   * the weighted keys of a state: by_new a^(C-1-j) z_j in three parts (24 bits): states come out as exact as fp32 sums make them
+//   * the state, where it is read: two parts (16 bits), three for fp32
+//   * the weighted scores P: one part for bf16 (an error like the output's own rounding), two for f16, three for fp32
+// and products of parts that together lie below what is kept are left out (kOrder).
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short  s16x4 __attribute__((ext_vector_type(4)));
+typedef short  s16x8 __attribute__((ext_vector_type(8)));
+typedef float  f32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int parts_of(int dt) { return dt == kBF16 ? 1 : dt == kF16 ? 2 : 3; }
+// Tokens of a block: what LDS holds of X, Y and Z next to each other.
+constexpr int block_tokens(int dt, int ap) { return dt == kF32 || (dt == kF16 && ap > 128) ? 32 : 64; }
+
+template <int N> struct Parts { bf16x8 p[N]; };
+
+// The first N bf16 parts of x: x = part 0 + part 1 + ..., each the rounding of what the ones before leave.
+template <int N> __device__ __forceinline__ void split(float x, bf16_t (&p)[N])
+{
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        p[n] = (bf16_t)x;
+        x -= (float)p[n];
+    }
+}
+// acc += a b for sums of parts: all products a[i] b[j] with i + j < kOrder.
+template <int kOrder, int NA, int NB> __device__ __forceinline__ f32x4 product(const Parts<NA> &a, const Parts<NB> &b, f32x4 acc)
+{
+#pragma unroll
+    for (int i = NA - 1; i >= 0; --i)
+#pragma unroll
+        for (int j = NB - 1; j >= 0; --j)
+            if (i + j < kOrder) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[j], acc, 0, 0, 0);
+    return acc;
+}
+
+// Tiles in LDS are rows of COLS bf16 whose 16-byte granules are permuted within each row by an exclusive or with a number made of the row.  The
+// permutation keeps both kinds of reading free of bank conflicts: the same granule of 16 consecutive rows (row operands), and four
+// granules of four consecutive rows (operands read transposed).
+template <int COLS> struct Tile {
+    static constexpr int kGranules = COLS / 8;
+    __device__ __forceinline__ static int swizzle(int row)
+    {
+        if constexpr (kGranules >= 16) return (row & 3) << 2 | ((row >> 2) & 3);
+        else if constexpr (kGranules == 8) return ((row >> 1) & 1) << 2 | ((row >> 2) & 3);
+        else return (row >> 2) & 3;
+    }
+    __device__ __forceinline__ static int at(int row, int col) { return row * COLS + ((((col >> 3) ^ swizzle(row)) << 3) | (col & 7)); }
+};
+
+// Reads the transposed operand: lane l of group g receives tile[row][column of lane l] for the eight rows row0 + 8 g .. + 7.  The
+// instruction hands lane l of 16 the l-th column of the four rows whose 16 pieces of four columns the 16 lanes point at: lane s at row s / 4, piece
+// s % 4, which starts at column col0 + piece * (s % 4).
+__device__ __forceinline__ s16x4 read_transposed(const bf16_t *p)
+{
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)p);
+}
+template <int COLS> __device__ __forceinline__ bf16x8 column_operand(const bf16_t *tile, int row0, int col0, int piece, int lane)
+{
+    const int row = row0 + 8 * (lane >> 4) + ((lane & 15) >> 2), col = col0 + piece * (lane & 3);
+    const s16x4 a = read_transposed(tile + Tile<COLS>::at(row, col)), b = read_transposed(tile + Tile<COLS>::at(row + 4, col));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+// Lane l of group g receives the eight columns k0 + 8 g .. + 7 of row row0 + l.
+template <int COLS> __device__ __forceinline__ bf16x8 row_operand(const bf16_t *tile, int row0, int k0, int lane)
+{
+    return *(const bf16x8 *)(tile + Tile<COLS>::at(row0 + (lane & 15), k0 + 8 * (lane >> 4)));
+}
+
+// A block of tokens on its way from memory to LDS: C rows of COLS elements, eight at a time, spread over THREADS lanes.
+template <int DT, int C, int COLS, int THREADS> struct Stage {
+    typedef typename Elem<DT>::T T;
+    static constexpr int kItems = C * COLS / 8, kEach = (kItems + THREADS - 1) / THREADS, kQuads = sizeof(T) / 2;
+    u32x4 v[kEach][kQuads];
+
+    // Row i of the block is at p + i * step; rows from n on and columns from `cols` on are zeros.  `whole`: granules of eight elements are
+    // aligned and either inside or outside.
+    __device__ __forceinline__ void load(const T *p, long long step, int n, int cols, bool whole)
+    {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int item = i * THREADS + (int)threadIdx.x, row = item / (COLS / 8), col = item % (COLS / 8) * 8;
+            const bool there = item < kItems && row < n && col < cols;
+#pragma unroll
+            for (int q = 0; q < kQuads; ++q) v[i][q] = u32x4{0u, 0u, 0u, 0u};
+            if (!there) continue;
+            const T *src = p + row * step + col;
+            if (whole) {
+#pragma unroll
+                for (int q = 0; q < kQuads; ++q) v[i][q] = ((const u32x4 *)src)[q];
+            } else {
+                T e[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) e[k] = col + k < cols ? src[k] : (T)0.0f;
+                __builtin_memcpy(&v[i][0], e, sizeof e);
+            }
+        }
+    }
+    __device__ __forceinline__ void store(bf16_t *tile) const                     // the parts are C * COLS elements apart
+    {
+        constexpr int N = parts_of(DT);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int item = i * THREADS + (int)threadIdx.x, row = item / (COLS / 8), col = item % (COLS / 8) * 8;
+            if (item >= kItems) break;
+            bf16_t *to = tile + Tile<COLS>::at(row, col);
+            if constexpr (N == 1) {
+                *(u32x4 *)to = v[i][0];
+            } else {
+                T e[8];
+                __builtin_memcpy(e, &v[i][0], sizeof e);
+                bf16x8 part[N];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    bf16_t p[N];
+                    split<N>((float)e[k], p);
+#pragma unroll
+                    for (int n = 0; n < N; ++n) part[n][k] = p[n];
+                }
+#pragma unroll
+                for (int n = 0; n < N; ++n) *(bf16x8 *)(to + n * C * COLS) = part[n];
+            }
+        }
+    }
+};
+
+// Which piece of which row a workgroup walks over.  Rows are cut into segments of 2^segment_log2 tokens; the segments of row r have the numbers
+// from offsets[r] / 2^segment_log2 + r on, which leaves every row room for its own without anything being counted first.
+struct Piece {
+    unsigned r;
+    long long lo, hi;                              // the row's tokens
+    long long first, end;                          // the segment's, counted from where the walk starts
+    bool last;
+};
+__device__ __forceinline__ bool find_piece(const WalkArgs &W, unsigned number, Piece &p)
+{
+    unsigned lo = 0, hi = W.rows;
+    const bool one = (W.total >> W.segment_log2) == 0;       // a row is one segment
+    if (one) {
+        lo = number;
+    } else {
+        while (hi - lo > 1) {                      // the last row whose segments start at or below `number`
+            const unsigned mid = lo + (hi - lo) / 2;
+            if ((W.offsets[mid] >> W.segment_log2) + mid <= (long long)number) lo = mid; else hi = mid;
+        }
+    }
+    p.r = lo;
+    row_extent(W.offsets, p.r, W.total, p.lo, p.hi);
+    const long long length = p.hi - p.lo, s = one ? 0 : (long long)number - (p.lo >> W.segment_log2) - p.r, segment = 1ll << W.segment_log2;
+    p.first = s * segment;
+    if (s < 0 || (s > 0 && p.first >= length)) return false;
+    p.end = p.first + segment < length ? p.first + segment : length;
+    p.last = p.end == length;
+    return true;
+}
+
+// Four consecutive columns of the output.  `whole`: they are aligned and all inside or all outside.
+template <class T> __device__ __forceinline__ void store_four(T *row, int col, int cols, f32x4 v, float by, bool whole)
+{
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    if (whole) {
+        if (col < cols) *(T4 *)(row + col) = T4{(T)(v[0] * by), (T)(v[1] * by), (T)(v[2] * by), (T)(v[3] * by)};
+    } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (col + r < cols) row[col + r] = (T)(v[r] * by);
+    }
+}
+
+template <int DT, int AP, int WAVES> __global__ __launch_bounds__(64 * WAVES) void walk_kernel(WalkArgs W)
 {
     typedef typename Elem<DT>::T T;
-    typedef typename Elem<DO>::T O;
-    __shared__ float m[kMaxDim][64];
-    const unsigned blocks = (W.E + 63) / 64;
-    const unsigned e = blockIdx.x % blocks * 64 + threadIdx.x, h = blockIdx.x / blocks % W.heads, r = blockIdx.x / blocks / W.heads;
-    const int col = threadIdx.x;
+    constexpr int N = parts_of(DT), C = block_tokens(DT, AP), EB = 16 * WAVES, kThreads = 64 * WAVES;
+    constexpr int kTiles = C / 16, kSteps = C / 32, kOrder = N == 3 ? 3 : 2;       // tiles of 16 tokens, steps of 32
+    __shared__ __attribute__((aligned(16))) bf16_t sx[N * C * AP], sy[N * C * AP], sz[N * C * EB], sp[N * C * C];
+    __shared__ __attribute__((aligned(16))) float weight[C];
+
+    const unsigned blocks = (W.E + EB - 1) / EB;
+    const unsigned block = blockIdx.x % blocks, h = blockIdx.x / blocks % W.heads, number = blockIdx.x / blocks / W.heads;
+    const int lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    if (block == 0 && h == 0)                      // offsets and slots are looked over once
+        for (size_t r = (size_t)number * kThreads + threadIdx.x; r < W.rows; r += (size_t)W.pieces * kThreads) {
+            const long long a = W.offsets[r], b = W.offsets[r + 1];
+            if (a < 0 || b < a || b > W.total || (W.slots && W.slots[r] >= W.states)) raise_fault(W.ws, kFaultBadIndex);
+        }
+    Piece piece;
+    if (!find_piece(W, number, piece)) return;
+    const bool reads = W.out.data != nullptr;
+    if (!reads && piece.last) return;              // (what a row's last segment adds, nobody asks for)
+
+    const float log_decay = W.log_decay[h];
+    const int e0 = (int)block * EB;                // the workgroup's first column
+    const unsigned e = e0 + 16 * wave + l;         // the lane's
+    const bool column = e < W.E;
+    const long long slot = state_of(W.slots, piece.r, W.states);
+    const size_t state = ((size_t)slot * W.heads + h) * W.A * W.E, between = ((size_t)number * W.heads + h) * W.A * W.E;
+
+    // M[2 s + t][r] is M[a][e] with a = 32 s + 8 g + 4 t + r
+    f32x4 M[AP / 16];
+    {
+        // a row of several segments finds what it starts from in the workspace, also for the first of them
+        const float *from = !reads ? nullptr : piece.first > 0 || !piece.last ? W.between + between : W.m_in && slot >= 0 ? W.m_in + state : nullptr;
+        const bool own = reads && (piece.first > 0 || !piece.last);
+#pragma unroll
+        for (int t = 0; t < AP / 16; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const unsigned a = 32 * (t / 2) + 8 * g + 4 * (t & 1) + r;
+                M[t][r] = from && column && a < W.A ? from[own ? (size_t)a * W.E + e : (size_t)a * W.m_a + (size_t)e * W.m_e] : 0.0f;
+            }
+    }
+    float reading[kTiles];                         // a^(i+1), from the end a^i, of the lane's token in each tile
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) reading[t] = decay_power(log_decay, (float)(16 * t + l + (W.from_end ? 0 : 1)));
+    if (reads)                                     // P above its diagonal of tiles: zeros for good
+        for (int i = threadIdx.x; i < N * (C / 32) * 16 * 2; i += kThreads) {
+            const int n = i / (C / 32 * 32), t = i / 32 % (C / 32), row = i / 2 % 16, half = i % 2;
+            *(u32x4 *)(sp + n * C * C + Tile<C>::at(32 * t + row, 32 * t + 16 + 8 * half)) = u32x4{0u, 0u, 0u, 0u};
+        }
+
+    const long long sign = W.from_end ? -1 : 1, origin = W.from_end ? piece.hi - 1 : piece.lo;
+    const T *x = (const T *)W.x.data + W.x.at(h, W.heads), *y = (const T *)W.y.data + W.y.at(h, W.heads), *z = (const T *)W.z.data + W.z.at(h, W.heads) + e0;
+    const int ecols = (int)W.E - e0;
+    Stage<DT, C, AP, kThreads> next_x, next_y;
+    Stage<DT, C, EB, kThreads> next_z;
+    auto fetch = [&](long long at) {
+        const int n = (int)(piece.end - at < C ? piece.end - at : C);
+        const long long t = origin + sign * at;
+        if (reads) next_x.load(x + t * W.x.token, sign * W.x.token, n, (int)W.A, W.whole & 1);
+        next_y.load(y + t * W.y.token, sign * W.y.token, n, (int)W.A, W.whole & 2);
+        next_z.load(z + t * W.z.token, sign * W.z.token, n, ecols, W.whole & 4);
+    };
+    if (piece.first < piece.end) fetch(piece.first);
+    for (long long at = piece.first; at < piece.end; at += C) {
+        const int n = (int)(piece.end - at < C ? piece.end - at : C);
+        if (reads) next_x.store(sx);
+        next_y.store(sy);
+        next_z.store(sz);
+        if ((int)threadIdx.x < C)
+            weight[threadIdx.x] = (int)threadIdx.x < n ? W.by_new * decay_power(log_decay, (float)(n - 1 - (int)threadIdx.x + (W.from_end ? 1 : 0))) : 0.0f;
+        __syncthreads();
+        if (at + C < piece.end) fetch(at + C);
+
+        if (reads) {
+            // P^T, 16 keys by 16 queries at a time
+#pragma unroll
+            for (int k = 0; k < (kTiles * (kTiles + 1) / 2 + WAVES - 1) / WAVES; ++k) {
+                const int tile = wave + k * WAVES;
+                if (tile >= kTiles * (kTiles + 1) / 2) break;
+                const int it = tile >= 6 ? 3 : tile >= 3 ? 2 : tile >= 1 ? 1 : 0, jt = tile - it * (it + 1) / 2;
+                f32x4 p = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int s = 0; s < AP / 32; ++s) {
+                    Parts<N> a, b;
+#pragma unroll
+                    for (int m = 0; m < N; ++m) {
+                        a.p[m] = row_operand<AP>(sy + m * C * AP, 16 * jt, 32 * s, lane);
+                        b.p[m] = row_operand<AP>(sx + m * C * AP, 16 * it, 32 * s, lane);
+                    }
+                    p = product<kOrder>(a, b, p);
+                }
+                const int i = 16 * it + l, j = 16 * jt + 4 * g;
+                bf16_t parts[4][N];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) split<N>(j + r <= i ? p[r] * (W.by_new * decay_power(log_decay, (float)(i - j - r))) : 0.0f, parts[r]);
+#pragma unroll
+                for (int m = 0; m < N; ++m) {
+                    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+                    *(bf16x4 *)(sp + m * C * C + Tile<C>::at(i, j)) = bf16x4{parts[0][m], parts[1][m], parts[2][m], parts[3][m]};
+                }
+            }
+            __syncthreads();
+        }
+        Parts<N> zt[kSteps];                       // 16 columns of Z by 32 tokens
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+            for (int m = 0; m < N; ++m) zt[s].p[m] = column_operand<EB>(sz + m * C * EB, 32 * s, 16 * wave, 4, lane);
+        if (reads) {
+            constexpr int NM = N == 3 ? 3 : 2;
+            f32x4 o[kTiles];
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) o[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int s = 0; s < AP / 32; ++s) {
+                Parts<NM> m;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    bf16_t part[NM];
+                    split<NM>(M[2 * s + k / 4][k % 4], part);
+#pragma unroll
+                    for (int i = 0; i < NM; ++i) m.p[i][k] = part[i];
+                }
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) {
+                    Parts<N> b;
+#pragma unroll
+                    for (int i = 0; i < N; ++i) b.p[i] = row_operand<AP>(sx + i * C * AP, 16 * t, 32 * s, lane);
+                    o[t] = product<kOrder>(m, b, o[t]);
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[t][r] *= reading[t];
+#pragma unroll
+                for (int s = 0; s <= t / 2; ++s) {
+                    Parts<N> b;
+#pragma unroll
+                    for (int i = 0; i < N; ++i) b.p[i] = row_operand<C>(sp + i * C * C, 16 * t, 32 * s, lane);
+                    o[t] = product<kOrder>(zt[s], b, o[t]);
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) {
+                if (16 * t + l >= n) continue;
+                const long long token = origin + sign * (at + 16 * t + l);
+                const int col = e0 + 16 * wave + 4 * g;
+                if (W.wide) store_four((float *)W.out.data + W.out.at(h, W.heads) + token * W.out.token, col, (int)W.E, o[t], W.by_read, W.whole & 8);
+                else store_four((T *)W.out.data + W.out.at(h, W.heads) + token * W.out.token, col, (int)W.E, o[t], W.by_read, W.whole & 8);
+            }
+        }
+        // the state
+        const Decay decay(log_decay, (float)n);
+#pragma unroll
+        for (int t = 0; t < AP / 16; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) M[t][r] = decay(M[t][r]);
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            Parts<3> wz;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                float v = 0.0f;
+#pragma unroll
+                for (int m = N - 1; m >= 0; --m) v += (float)zt[s].p[m][k];
+                bf16_t part[3];
+                split<3>(v * weight[32 * s + 8 * g + k], part);
+#pragma unroll
+                for (int i = 0; i < 3; ++i) wz.p[i][k] = part[i];
+            }
+#pragma unroll
+            for (int t = 0; t < AP / 16; ++t) {
+                Parts<N> yt;
+#pragma unroll
+                for (int m = 0; m < N; ++m) yt.p[m] = column_operand<AP>(sy + m * C * AP, 32 * s, 32 * (t / 2) + 4 * (t & 1), 8, lane);
+                M[t] = product<3>(yt, wz, M[t]);
+            }
+        }
+        __syncthreads();
+    }
+    float *to = !reads ? W.between + between : piece.last && W.m_out && slot >= 0 ? W.m_out + state : nullptr;
+    if (to && column)
+#pragma unroll
+        for (int t = 0; t < AP / 16; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const unsigned a = 32 * (t / 2) + 8 * g + 4 * (t & 1) + r;
+                if (a < W.A) to[!reads ? (size_t)a * W.E + e : (size_t)a * W.m_a + (size_t)e * W.m_e] = M[t][r];
+            }
+}
+
+// What each segment of a row starts from, from what the segments in front of it add: a thread takes one element of the state along the row.
+constexpr int kJoinThreads = 256;
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(WalkArgs W)
+{
+    const unsigned size = W.A * W.E, blocks = (size + kJoinThreads - 1) / kJoinThreads;
+    const unsigned i = blockIdx.x % blocks * kJoinThreads + threadIdx.x, h = blockIdx.x / blocks % W.heads, r = blockIdx.x / blocks / W.heads;
+    if (i >= size) return;
     long long lo, hi;
     row_extent(W.offsets, r, W.total, lo, hi);
-    if (threadIdx.x == 0) {
-        const long long a = W.offsets[r], b = W.offsets[r + 1];
-        if (a < 0 || b < a || b > W.total) raise_fault(W.ws, kFaultBadIndex);
-        if (W.slots && W.slots[r] >= W.states) raise_fault(W.ws, kFaultBadIndex);
-    }
-    if (e >= W.E) return;                          // (lanes work on columns of their own; nothing is waited for)
+    const long long segment = 1ll << W.segment_log2, segments = (hi - lo + segment - 1) >> W.segment_log2, first = (lo >> W.segment_log2) + r;
+    if (segments <= 1 || first + segments > (long long)W.pieces) return;
     const long long slot = state_of(W.slots, r, W.states);
-    const size_t state = ((size_t)slot * W.heads + h) * W.A * W.E;
-    for (unsigned a = 0; a < W.A; ++a) m[a][col] = W.m_in && slot >= 0 ? W.m_in[state + (size_t)a * W.m_a + (size_t)e * W.m_e] : 0.0f;
-    const Decay decay(W.log_decay[h], 1.0f);
-    const T *x = (const T *)W.x.data + W.x.at(h, W.heads), *y = (const T *)W.y.data + W.y.at(h, W.heads), *z = (const T *)W.z.data + W.z.at(h, W.heads);
-    O *out = (O *)W.out.data + W.out.at(h, W.heads);
-    for (long long i = 0; i < hi - lo; ++i) {
-        const long long t = W.from_end ? hi - 1 - i : lo + i;
-        const T *xt = x + t * W.x.token, *yt = y + t * W.y.token;
-        const float zt = (float)z[t * W.z.token + e] * W.by_new;
-        float sum = 0.0f;
-        for (unsigned a = 0; a < W.A; ++a) {
-            float v = m[a][col];
-            if (!W.from_end) v = decay(v);
-            v += (float)yt[a] * zt;
-            sum += (float)xt[a] * v;
-            if (W.from_end) v = decay(v);
-            m[a][col] = v;
-        }
-        out[t * W.out.token + e] = (O)(sum * W.by_read);
+    const unsigned a = i / W.E, e = i % W.E;
+    float m = W.m_in && slot >= 0 ? W.m_in[((size_t)slot * W.heads + h) * size + (size_t)a * W.m_a + (size_t)e * W.m_e] : 0.0f;
+    const Decay decay(W.log_decay[h], (float)segment);
+    float *p = W.between + ((size_t)first * W.heads + h) * size + i;
+    const size_t step = (size_t)W.heads * size;
+    for (long long s = 0; s + 1 < segments; ++s, p += step) {
+        const float added = *p;
+        *p = m;
+        m = decay(m) + added;
     }
-    if (W.m_out && slot >= 0)
-        for (unsigned a = 0; a < W.A; ++a) W.m_out[state + (size_t)a * W.m_a + (size_t)e * W.m_e] = m[a][col];
+    *p = m;
 }
 
 // out[t][stored head][i] = the sum of part[t][head][i] over the heads that share the stored head.
@@ -182,8 +549,6 @@ bool launch(const void *fn, size_t grid, unsigned block, void *args, hipStream_t
 }
 
 template <template <int> class Pick> const void *pick(int dt) { return dt == kF16 ? Pick<kF16>::fn() : dt == kF32 ? Pick<kF32>::fn() : Pick<kBF16>::fn(); }
-template <int DT> struct WalkSame { static const void *fn() { return (const void *)walk_kernel<DT, DT>; } };
-template <int DT> struct WalkWide { static const void *fn() { return (const void *)walk_kernel<DT, kF32>; } };
 template <int DT> struct SumHeads { static const void *fn() { return (const void *)sum_heads_kernel<DT>; } };
 template <int DT> struct Step { static const void *fn() { return (const void *)step_kernel<DT>; } };
 
@@ -199,15 +564,32 @@ tcuscan_status_t check_shape(const tcuscan_attention_shape_t *p, int dt)
     for (long long shared : {s.q_heads, s.k_heads, s.v_heads})
         if (shared < 1 || shared > s.heads || s.heads % shared) return TCUSCAN_ERR_INVALID_ARG;
     if (s.dk > kMaxDim || s.dv > kMaxDim) return TCUSCAN_ERR_UNSUPPORTED;
+    if (s.total >> 40) return TCUSCAN_ERR_UNSUPPORTED;
     if (s.rows > 0x3FFFFFFF || s.heads > 0xFFFF || (unsigned long long)s.rows * s.heads > kMostBlocks / 8) return TCUSCAN_ERR_UNSUPPORTED;
     return TCUSCAN_OK;
 }
 
+// Rows are cut into segments so that a call with few rows and heads still has a workgroup or two for every compute unit.
+constexpr size_t kWantedGroups = 512;
+constexpr unsigned kMinSegmentLog2 = 9, kWholeRows = 62;
+unsigned segment_log2_for(const tcuscan_attention_shape_t &s)
+{
+    const size_t blocks = (size_t)((s.dk > s.dv ? s.dk : s.dv) + 127) / 128;
+    unsigned log2 = kMinSegmentLog2;
+    while (((size_t)s.total * s.heads * blocks) >> log2 > kWantedGroups) ++log2;
+    return (size_t)s.total >> log2 ? log2 : kWholeRows;
+}
+size_t pieces_for(const tcuscan_attention_shape_t &s, unsigned segment_log2) { return (size_t)s.rows + ((size_t)s.total >> segment_log2); }
+
 struct Layout {
-    size_t part, all;
+    size_t between, part, all;
+    unsigned segment_log2;
     Layout(const tcuscan_attention_shape_t &s, bool backward)
     {
-        part = chain_layout::kHeaderBytes;
+        segment_log2 = segment_log2_for(s);
+        between = chain_layout::kHeaderBytes;
+        part = between + (segment_log2 == kWholeRows ? 0 : pieces_for(s, segment_log2) * s.heads * s.dk * s.dv * 4);
+        part = (part + 255) / 256 * 256;
         size_t wide = 0;
         if (backward) {
             if (s.q_heads < s.heads || s.k_heads < s.heads) wide = (size_t)s.dk;
@@ -221,17 +603,44 @@ bool misaligned(const void *p, size_t to) { return (uintptr_t)p % to != 0; }
 
 Heads heads_of(const void *data, long long token, long long head, long long heads) { return {(void *)data, token, head, (unsigned)heads}; }
 
+template <int DT, int WAVES> const void *walk_for(unsigned A)
+{
+    return A <= 32 ? (const void *)walk_kernel<DT, 32, WAVES> : A <= 64 ? (const void *)walk_kernel<DT, 64, WAVES>
+         : A <= 128 ? (const void *)walk_kernel<DT, 128, WAVES> : (const void *)walk_kernel<DT, 256, WAVES>;
+}
+template <int WAVES> const void *walk_for(int dt, unsigned A) { return dt == kF16 ? walk_for<kF16, WAVES>(A) : dt == kF32 ? walk_for<kF32, WAVES>(A) : walk_for<kBF16, WAVES>(A); }
+
+// Whether groups of `n` elements of every token's features are aligned and whole.
+bool whole(const Heads &x, unsigned dims, size_t esz, unsigned n)
+{
+    const size_t bytes = n * esz < 16 ? n * esz : 16;
+    return dims % n == 0 && (uintptr_t)x.data % bytes == 0 && (size_t)x.token * esz % bytes == 0 && (size_t)x.head * esz % bytes == 0;
+}
+
 // One walk, into `out`; with heads that share the output, into `part` first.
 tcuscan_status_t walk(WalkArgs W, Heads out, float *part, int dt, hipStream_t s)
 {
-    const size_t grid = (size_t)W.rows * W.heads * ((W.E + 63) / 64);
+    const size_t esz = elem_bytes(dt);
+    const unsigned waves = W.E <= 64 ? 4 : 8;
+    const size_t groups = (size_t)W.pieces * W.heads * ((W.E + 16 * waves - 1) / (16 * waves));
+    const size_t join_groups = (size_t)W.rows * W.heads * (((size_t)W.A * W.E + kJoinThreads - 1) / kJoinThreads);
+    if (groups > kMostBlocks || join_groups > kMostBlocks) return TCUSCAN_ERR_UNSUPPORTED;
     const bool shared = out.heads < W.heads;
-    W.out = shared ? Heads{part, (long long)W.heads * W.E, W.E, W.heads} : out;
-    if (!launch(shared ? pick<WalkWide>(dt) : pick<WalkSame>(dt), grid, 64, &W, s)) return TCUSCAN_ERR_HIP;
-    if (!shared) return TCUSCAN_OK;
-    SumArgs S = {part, out, W.total, W.heads, W.E};
+    const Heads to = shared ? Heads{part, (long long)W.heads * W.E, W.E, W.heads} : out;
+    W.wide = shared;
+    W.whole = whole(W.x, W.A, esz, 8) | whole(W.y, W.A, esz, 8) << 1 | whole(W.z, W.E, esz, 8) << 2 | whole(to, W.E, shared ? 4 : esz, 4) << 3;
+    const void *fn = waves == 4 ? walk_for<4>(dt, W.A) : walk_for<8>(dt, W.A);
+    if (W.segment_log2 != kWholeRows) {
+        W.out = Heads{};
+        if (!launch(fn, groups, 64 * waves, &W, s) || !launch((const void *)join_kernel, join_groups, kJoinThreads, &W, s)) return TCUSCAN_ERR_HIP;
+    }
+    W.out = to;
+    if (!W.out.data) W.out.data = W.ws;            // (no tokens: nothing is written there)
+    if (!launch(fn, groups, 64 * waves, &W, s)) return TCUSCAN_ERR_HIP;
     const size_t items = (size_t)W.total * out.heads * W.E;
-    if (!items) return TCUSCAN_OK;
+    if (!shared || !items) return TCUSCAN_OK;
+    SumArgs S = {part, out, W.total, W.heads, W.E};
+    if ((items + kSumThreads - 1) / kSumThreads > kMostBlocks) return TCUSCAN_ERR_UNSUPPORTED;
     return launch(pick<SumHeads>(dt), (items + kSumThreads - 1) / kSumThreads, kSumThreads, &S, s) ? TCUSCAN_OK : TCUSCAN_ERR_HIP;
 }
 
@@ -267,6 +676,7 @@ tcuscan_status_t tcuscan_decay_attention(const tcuscan_attention_shape_t *shape,
     W.y = heads_of(d_k, p.k_token, p.k_head, p.k_heads);
     W.z = heads_of(d_v, p.v_token, p.v_head, p.v_heads);
     W.log_decay = d_log_decay; W.offsets = d_offsets; W.slots = d_slots; W.m_in = d_state_in; W.m_out = d_state_out; W.ws = d_ws;
+    W.between = (float *)((char *)d_ws + L.between); W.segment_log2 = L.segment_log2; W.pieces = (unsigned)pieces_for(p, L.segment_log2);
     W.states = (long long)states; W.total = p.total; W.rows = (unsigned)p.rows; W.heads = (unsigned)p.heads;
     W.A = (unsigned)p.dk; W.E = (unsigned)p.dv; W.m_a = W.E; W.m_e = 1;
     W.by_new = 1.0f; W.by_read = scale; W.from_end = 0;
@@ -305,6 +715,7 @@ tcuscan_status_t tcuscan_decay_attention_backward(const tcuscan_attention_shape_
                 v = heads_of(d_v, p.v_token, p.v_head, p.v_heads), o = heads_of(d_out_grad, p.o_token, p.o_head, p.heads);
     WalkArgs W = {};
     W.log_decay = d_log_decay; W.offsets = d_offsets; W.ws = d_ws;
+    W.between = (float *)((char *)d_ws + L.between); W.segment_log2 = L.segment_log2; W.pieces = (unsigned)pieces_for(p, L.segment_log2);
     W.states = p.rows; W.total = p.total; W.rows = (unsigned)p.rows; W.heads = (unsigned)p.heads;
     const unsigned dk = (unsigned)p.dk, dv = (unsigned)p.dv;
     // dq, with the states of the forward pass
