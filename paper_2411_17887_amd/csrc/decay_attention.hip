@@ -508,7 +508,8 @@ template <int DT> __global__ __launch_bounds__(kSumThreads) void sum_heads_kerne
     ((T *)S.out.data)[t * S.out.token + (long long)h * S.out.head + d] = (T)sum;
 }
 
-// One token for each of many sequences: a workgroup per (sequence, head), lanes along the state's rows (dv).
+// One token for each of many sequences.  A workgroup takes a block of columns of one state: 2^lanes_log2 lanes to a row, VEC columns each, as many rows at
+// a time as the workgroup has lanes for.  The state is read and written once; nothing else counts.
 struct StepArgs {
     Heads q, k, v, out;
     const float *log_decay;
@@ -516,30 +517,73 @@ struct StepArgs {
     float *state;
     void *ws;
     long long states;
-    unsigned n, heads, A, E;
+    unsigned n, heads, A, E, blocks, lanes_log2;
     float scale;
 };
-template <int DT> __global__ __launch_bounds__(256) void step_kernel(StepArgs S)
+constexpr int kStepThreads = 256;
+template <int DT, int VEC> __global__ __launch_bounds__(kStepThreads) void step_kernel(StepArgs S)
 {
     typedef typename Elem<DT>::T T;
-    const unsigned h = blockIdx.x % S.heads, i = blockIdx.x / S.heads;
+    typedef float Vec __attribute__((ext_vector_type(VEC)));
+    __shared__ float ks[kMaxDim], qs[kMaxDim];
+    __shared__ Vec sums[kStepThreads / 64][64];
+    const unsigned block = blockIdx.x % S.blocks, h = blockIdx.x / S.blocks % S.heads, i = blockIdx.x / S.blocks / S.heads;
+    const unsigned lanes = 1u << S.lanes_log2, e = (block * lanes + (threadIdx.x & (lanes - 1))) * VEC, row0 = threadIdx.x >> S.lanes_log2, rows = kStepThreads >> S.lanes_log2;
     const long long slot = state_of(S.slots, i, S.states);
-    if (threadIdx.x == 0 && S.slots && S.slots[i] >= S.states) raise_fault(S.ws, kFaultBadIndex);
+    if (threadIdx.x == 0 && block == 0 && h == 0 && S.slots && S.slots[i] >= S.states) raise_fault(S.ws, kFaultBadIndex);
+    const bool column = e < S.E, there = slot >= 0;
+    float *m = S.state + ((size_t)(there ? slot : 0) * S.heads + h) * S.A * S.E + e;
+    constexpr unsigned kAhead = 8;
+    Vec s[kAhead];
+    // the first rows are on their way before anything else is looked at
+    auto load = [&](unsigned a0) {
+#pragma unroll
+        for (unsigned u = 0; u < kAhead; ++u) {
+            const unsigned a = a0 + u * rows;
+            s[u] = Vec{};
+            if (there && column && a < S.A) s[u] = *(const Vec *)(m + (size_t)a * S.E);
+        }
+    };
+    load(row0);
     const T *q = (const T *)S.q.data + S.q.at(h, S.heads) + i * S.q.token, *k = (const T *)S.k.data + S.k.at(h, S.heads) + i * S.k.token,
             *v = (const T *)S.v.data + S.v.at(h, S.heads) + i * S.v.token;
-    T *out = (T *)S.out.data + S.out.at(h, S.heads) + i * S.out.token;
-    const unsigned e = threadIdx.x;
-    if (e >= S.E) return;
-    const Decay decay(S.log_decay[h], 1.0f);
-    const float ve = (float)v[e];
-    float sum = 0.0f;
-    float *m = S.state + ((size_t)(slot < 0 ? 0 : slot) * S.heads + h) * S.A * S.E + e;
-    for (unsigned a = 0; a < S.A; ++a) {
-        const float old = slot < 0 ? 0.0f : m[(size_t)a * S.E], s = decay(old) + (float)k[a] * ve;
-        if (slot >= 0) m[(size_t)a * S.E] = s;
-        sum += (float)q[a] * s;
+    for (unsigned a = threadIdx.x; a < S.A; a += kStepThreads) {
+        ks[a] = (float)k[a];
+        qs[a] = (float)q[a];
     }
-    out[e] = (T)(sum * S.scale);
+    Vec ve = {}, sum = {};
+#pragma unroll
+    for (int c = 0; c < VEC; ++c)
+        if (e + c < S.E) ve[c] = (float)v[e + c];
+    const Decay decay(S.log_decay[h], 1.0f);
+    __syncthreads();
+    for (unsigned a0 = row0; a0 < S.A; a0 += kAhead * rows) {
+        if (a0 != row0) load(a0);
+#pragma unroll
+        for (unsigned u = 0; u < kAhead; ++u) {
+            const unsigned a = a0 + u * rows;
+            if (a >= S.A) break;
+#pragma unroll
+            for (int c = 0; c < VEC; ++c) {
+                s[u][c] = fmaf(ks[a], ve[c], decay(s[u][c]));
+                sum[c] = fmaf(qs[a], s[u][c], sum[c]);
+            }
+            if (there && column) *(Vec *)(m + (size_t)a * S.E) = s[u];
+        }
+    }
+    // over the rows: lanes of a wavefront that have the same columns, then the wavefronts
+#pragma unroll
+    for (int c = 0; c < VEC; ++c)
+        for (unsigned d = lanes; d < 64; d *= 2) sum[c] += __shfl_xor(sum[c], (int)d);
+    sums[threadIdx.x >> 6][threadIdx.x & 63] = sum;
+    __syncthreads();
+    if (threadIdx.x >= lanes || !column) return;
+#pragma unroll
+    for (int w = 1; w < kStepThreads / 64; ++w) sum += sums[w][threadIdx.x];
+    T *out = (T *)S.out.data + S.out.at(h, S.heads) + i * S.out.token;
+#pragma unroll
+    for (int c = 0; c < VEC; ++c)
+        if (e + c < S.E) out[e + c] = (T)(sum[c] * S.scale);
 }
 
 bool launch(const void *fn, size_t grid, unsigned block, void *args, hipStream_t s)
@@ -550,7 +594,8 @@ bool launch(const void *fn, size_t grid, unsigned block, void *args, hipStream_t
 
 template <template <int> class Pick> const void *pick(int dt) { return dt == kF16 ? Pick<kF16>::fn() : dt == kF32 ? Pick<kF32>::fn() : Pick<kBF16>::fn(); }
 template <int DT> struct SumHeads { static const void *fn() { return (const void *)sum_heads_kernel<DT>; } };
-template <int DT> struct Step { static const void *fn() { return (const void *)step_kernel<DT>; } };
+template <int DT> struct Step { static const void *fn() { return (const void *)step_kernel<DT, 1>; } };
+template <int DT> struct StepByFour { static const void *fn() { return (const void *)step_kernel<DT, 4>; } };
 
 constexpr size_t kMostBlocks = 0x7FFFFFFFu;
 
@@ -747,10 +792,19 @@ tcuscan_status_t tcuscan_decay_attention_step(const tcuscan_attention_shape_t *s
     if (misaligned(d_q, esz) || misaligned(d_k, esz) || misaligned(d_v, esz) || misaligned(d_out, esz)) return TCUSCAN_ERR_INVALID_ARG;
     if (d_out == d_q || d_out == d_k || d_out == d_v || (!d_slots && states < (size_t)p.rows)) return TCUSCAN_ERR_INVALID_ARG;
     if (d_ws && (ws_bytes < chain_layout::kHeaderBytes || misaligned(d_ws, 8))) return TCUSCAN_ERR_WORKSPACE;
-    StepArgs S = {heads_of(d_q, p.q_token, p.q_head, p.q_heads), heads_of(d_k, p.k_token, p.k_head, p.k_heads), heads_of(d_v, p.v_token, p.v_head, p.v_heads),
-                  heads_of(d_out, p.o_token, p.o_head, p.heads), d_log_decay, d_slots, d_state, d_ws, (long long)states,
-                  (unsigned)p.rows, (unsigned)p.heads, (unsigned)p.dk, (unsigned)p.dv, scale};
-    return launch(pick<Step>(dt), (size_t)p.rows * p.heads, 256, &S, (hipStream_t)stream) ? TCUSCAN_OK : TCUSCAN_ERR_HIP;
+    StepArgs S = {};
+    S.q = heads_of(d_q, p.q_token, p.q_head, p.q_heads); S.k = heads_of(d_k, p.k_token, p.k_head, p.k_heads);
+    S.v = heads_of(d_v, p.v_token, p.v_head, p.v_heads); S.out = heads_of(d_out, p.o_token, p.o_head, p.heads);
+    S.log_decay = d_log_decay; S.slots = d_slots; S.state = d_state; S.ws = d_ws; S.states = (long long)states;
+    S.n = (unsigned)p.rows; S.heads = (unsigned)p.heads; S.A = (unsigned)p.dk; S.E = (unsigned)p.dv; S.scale = scale;
+    // lanes to a row: all of it, up to a wavefront; 128 bytes where there are few states, for more workgroups
+    const unsigned vec = S.E % 4 == 0 ? 4 : 1, row_lanes = (S.E + vec - 1) / vec;
+    const size_t all = (size_t)p.rows * p.heads;
+    while ((1u << S.lanes_log2) < row_lanes && S.lanes_log2 < 6) ++S.lanes_log2;
+    while (S.lanes_log2 > 3 && all * ((row_lanes + (1u << S.lanes_log2) - 1) >> S.lanes_log2) < kWantedGroups) --S.lanes_log2;
+    S.blocks = (row_lanes + (1u << S.lanes_log2) - 1) >> S.lanes_log2;
+    if (all * S.blocks > kMostBlocks) return TCUSCAN_ERR_UNSUPPORTED;
+    return launch(vec == 4 ? pick<StepByFour>(dt) : pick<Step>(dt), all * S.blocks, kStepThreads, &S, (hipStream_t)stream) ? TCUSCAN_OK : TCUSCAN_ERR_HIP;
 }
 
 }  // extern "C"

@@ -21,7 +21,7 @@ constexpr int kThreads = 256;
 struct LookupArgs {
     const void *ids, *weight;
     void *out, *ws;
-    size_t n, vocab, dim, weight_stride, out_stride;
+    size_t n, vocab, dim, weight_stride, out_stride, slices;
     float scale;
     int wide_ids;
 };
@@ -31,28 +31,90 @@ __device__ __forceinline__ long long id_at(const void *ids, int wide, size_t i)
     return wide ? ((const long long *)ids)[i] : (long long)((const int *)ids)[i];
 }
 
-// One wavefront per token.
-template <int DW, int DO> __global__ __launch_bounds__(kThreads) void lookup_kernel(LookupArgs A)
+// Columns of a row that one lane holds: a wavefront takes 64 * kLaneCols of them at a time.  ALIGNED: a lane's columns are next to each other and
+// load as whole granules; otherwise they are 64 apart, so that rows of any length and start load in runs of 64 elements.
+template <int DG> constexpr int kLaneCols = DG == kF32 ? 4 : 8;
+template <int DG, bool ALIGNED> struct Lane {
+    typedef typename Elem<DG>::T G;
+    static constexpr int N = kLaneCols<DG>, kSlice = 64 * N;
+    template <class X> using VecOf = X __attribute__((ext_vector_type(N)));
+    typedef VecOf<G> Vec;
+    static __device__ __forceinline__ size_t col(int lane, int k) { return ALIGNED ? (size_t)lane * N + k : (size_t)k * 64 + lane; }
+    // Columns of `row` from c0 on; those from `dim` on are zeros.  (ALIGNED: dim is a multiple of N.)
+    template <class X> static __device__ __forceinline__ VecOf<X> load(const X *row, size_t c0, size_t dim, int lane)
+    {
+        VecOf<X> v{};
+        if constexpr (ALIGNED) {
+            if (c0 + (size_t)lane * N < dim) v = *(const VecOf<X> *)(row + c0 + (size_t)lane * N);
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; ++k) v[k] = c0 + col(lane, k) < dim ? row[c0 + col(lane, k)] : (X)0.0f;
+        }
+        return v;
+    }
+    static __device__ __forceinline__ void add(float (&sum)[N], Vec v)
+    {
+#pragma unroll
+        for (int k = 0; k < N; ++k) sum[k] += (float)v[k];
+    }
+    // The finished row: scaled, added to what is there or not, rounded.
+    template <int DW> static __device__ __forceinline__ void finish(typename Elem<DW>::T *row, size_t c0, size_t dim, int lane, const float (&sum)[N], float scale, bool accumulate)
+    {
+        typedef typename Elem<DW>::T W;
+        if constexpr (ALIGNED) {
+            typedef W WVec __attribute__((ext_vector_type(N)));
+            if (c0 + (size_t)lane * N >= dim) return;
+            WVec *p = (WVec *)(row + c0 + (size_t)lane * N), w;
+            const WVec old = accumulate ? *p : WVec{};
+#pragma unroll
+            for (int k = 0; k < N; ++k) w[k] = (W)(accumulate ? fmaf(sum[k], scale, (float)old[k]) : sum[k] * scale);
+            *p = w;
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                const size_t c = c0 + col(lane, k);
+                if (c < dim) row[c] = (W)(accumulate ? fmaf(sum[k], scale, (float)row[c]) : sum[k] * scale);
+            }
+        }
+    }
+};
+
+// A wavefront takes a slice of the columns of kTokens tokens: their loads are on their way together.  (kTokens = 1: few tokens, whose columns are spread
+// over as many wavefronts as there are.)
+template <int DW, int DO, bool ALIGNED, int kTokens> __global__ __launch_bounds__(kThreads) void lookup_kernel(LookupArgs A)
 {
+    typedef Lane<DW == kF32 ? DO : DW, ALIGNED> L;             // (eight columns to a lane unless both types are fp32)
     typedef typename Elem<DW>::T W;
-    typedef typename Elem<DO>::T O;
-    const size_t t = (size_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
-    if (t >= A.n) return;
     const int lane = threadIdx.x & 63;
-    const long long id = id_at(A.ids, A.wide_ids, t);
-    const bool there = id >= 0 && id < (long long)A.vocab;
-    if (id >= (long long)A.vocab && lane == 0) raise_fault(A.ws, kFaultBadIndex);
-    const W *w = (const W *)A.weight + (there ? (size_t)id * A.weight_stride : 0);
-    O *o = (O *)A.out + t * A.out_stride;
-    for (size_t i = lane; i < A.dim; i += 64) o[i] = there ? (O)((float)w[i] * A.scale) : (O)0.0f;
+    const size_t item = (size_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6), t0 = item / A.slices * kTokens, c0 = item % A.slices * L::kSlice;
+    if (t0 >= A.n) return;
+    typename L::template VecOf<W> v[kTokens];
+#pragma unroll
+    for (int u = 0; u < kTokens; ++u) {
+        v[u] = typename L::template VecOf<W>{};
+        if (t0 + u >= A.n) break;
+        const long long id = id_at(A.ids, A.wide_ids, t0 + u);
+        if (id >= (long long)A.vocab) { if (c0 == 0 && lane == 0) raise_fault(A.ws, kFaultBadIndex); }
+        else if (id >= 0) v[u] = L::template load<W>((const W *)A.weight + (size_t)id * A.weight_stride, c0, A.dim, lane);
+    }
+#pragma unroll
+    for (int u = 0; u < kTokens; ++u) {
+        if (t0 + u >= A.n) break;
+        float f[L::N];
+#pragma unroll
+        for (int k = 0; k < L::N; ++k) f[k] = (float)v[u][k];
+        L::template finish<DO>((typename Elem<DO>::T *)A.out + (t0 + u) * A.out_stride, c0, A.dim, lane, f, A.scale, false);
+    }
 }
 
 struct GradArgs {
     const void *ids, *d_out;
     void *d_weight, *ws;
     uint32_t *keys, *tokens;
+    float *partial;
     size_t n, vocab, dim, out_stride, weight_stride;
     long long padding;
+    size_t piece, slices, piece_groups, rows;      // rows: of the table to a workgroup, where there are few tokens
     float scale;
     int wide_ids, accumulate;
 };
@@ -68,26 +130,185 @@ __global__ __launch_bounds__(kThreads) void token_keys_kernel(GradArgs A)
     A.tokens[t] = (uint32_t)t;
 }
 
-// One workgroup per row of the table.
-template <int DG, int DW> __global__ __launch_bounds__(kThreads) void row_sums_kernel(GradArgs A)
+// Few tokens: no sort.  A workgroup takes `rows` rows of the table, looks all token numbers over and keeps those of its rows in order; a
+// wavefront then sums a row at a time.  One launch.
+constexpr int kFewTokens = 4096, kMaxFewRows = 64;
+template <int DG, int DW, bool ALIGNED> __global__ __launch_bounds__(kThreads) void few_tokens_kernel(GradArgs A)
 {
-    typedef typename Elem<DG>::T G;
-    typedef typename Elem<DW>::T W;
-    const uint32_t row = blockIdx.x;
-    size_t lo = 0, hi = A.n;                                   // the first pair whose key is not below the row
-    while (lo < hi) {
-        const size_t mid = lo + (hi - lo) / 2;
-        if (A.keys[mid] < row) lo = mid + 1; else hi = mid;
+    typedef Lane<DG, ALIGNED> L;
+    typedef typename L::G G;
+    constexpr int kWaves = kThreads / 64;
+    __shared__ uint32_t list[kFewTokens];          // (row of the workgroup) << 16 | token, in the order of the tokens
+    __shared__ int counts[kWaves];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const size_t first = (size_t)blockIdx.x * A.rows;
+    int listed = 0;
+    for (size_t t0 = 0; t0 < A.n; t0 += kThreads) {
+        const size_t t = t0 + threadIdx.x;
+        const long long id = t < A.n ? id_at(A.ids, A.wide_ids, t) : -1;
+        if (blockIdx.x == 0 && id >= (long long)A.vocab) raise_fault(A.ws, kFaultBadIndex);
+        const bool mine = id >= (long long)first && id < (long long)(first + A.rows) && id < (long long)A.vocab && id != A.padding;
+        const uint64_t votes = __ballot(mine);
+        if (lane == 0) counts[wave] = __popcll(votes);
+        __syncthreads();
+        int at = listed, all = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            if (w < wave) at += counts[w];
+            all += counts[w];
+        }
+        if (mine) list[at + __popcll(votes & (((uint64_t)1 << lane) - 1))] = (uint32_t)(id - (long long)first) << 16 | (uint32_t)t;
+        listed += all;
+        __syncthreads();
     }
-    size_t end = lo;
-    while (end < A.n && A.keys[end] == row) ++end;
-    if (A.accumulate && lo == end) return;
-    W *w = (W *)A.d_weight + (size_t)row * A.weight_stride;
-    for (size_t i = threadIdx.x; i < A.dim; i += kThreads) {
+    const size_t last = first + A.rows < A.vocab ? first + A.rows : A.vocab;
+    for (size_t row = first + wave; row < last; row += kWaves) {
+        typename Elem<DW>::T *w = (typename Elem<DW>::T *)A.d_weight + row * A.weight_stride;
+        bool any = false;
+        for (size_t c0 = 0; c0 < A.dim; c0 += L::kSlice) {
+            float sum[L::N] = {};
+            for (int i0 = 0; i0 < listed; i0 += 64) {
+                const uint32_t item = i0 + lane < listed ? list[i0 + lane] : 0xFFFFFFFFu;
+                uint64_t votes = __ballot(item >> 16 == (uint32_t)(row - first));
+                any |= votes != 0;
+                while (votes) {                    // four rows of gradients on their way at a time
+                    const G *from[4];
+                    typename L::Vec v[4];
+                    int k = 0;
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const int source = votes ? __builtin_ctzll(votes) : -1;
+                        if (source >= 0) { votes &= votes - 1; k = u + 1; }
+                        from[u] = (const G *)A.d_out + (size_t)(__builtin_amdgcn_readlane((int)item, source < 0 ? 0 : source) & 0xFFFF) * A.out_stride;
+                    }
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+                        if (u < k) v[u] = L::load(from[u], c0, A.dim, lane);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+                        if (u < k) L::add(sum, v[u]);
+                }
+            }
+            if (any || !A.accumulate) L::template finish<DW>(w, c0, A.dim, lane, sum, A.scale, A.accumulate);
+        }
+    }
+}
+
+// Many tokens.  The sorted pairs are cut into pieces of `piece` pairs, whatever runs they hold, so that a frequent token's run is shared by many
+// wavefronts: a wavefront takes a piece and a slice of the columns.  Runs that lie inside a piece are finished there; what a piece has of
+// a run that goes on beyond it is kept, in fp32, in one of the piece's two places (0: the run comes from the piece before, 1: it starts here)
+// and added up, piece by piece in their order, by join_runs_kernel.  Workgroups behind the pieces' write zeros into rows that no token took.
+constexpr int kMaxPiece = 32, kZeroRows = 64;
+template <int DG, int DW, bool ALIGNED> __global__ __launch_bounds__(kThreads) void sum_runs_kernel(GradArgs A)
+{
+    typedef Lane<DG, ALIGNED> L;
+    typedef typename L::G G;
+    typedef typename Elem<DW>::T W;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (blockIdx.x >= A.piece_groups) {
+        __shared__ uint64_t taken;
+        const size_t first = (size_t)(blockIdx.x - A.piece_groups) * kZeroRows;
+        if (wave == 0) {
+            const uint32_t row = (uint32_t)first + lane;
+            size_t lo = 0, hi = A.n;               // the first pair whose key is not below the row
+            while (lo < hi) {
+                const size_t mid = lo + (hi - lo) / 2;
+                if (A.keys[mid] < row) lo = mid + 1; else hi = mid;
+            }
+            const uint64_t votes = __ballot(lo < A.n && A.keys[lo] == row);
+            if (lane == 0) taken = votes;
+        }
+        __syncthreads();
+        const float zeros[L::N] = {};
+        for (int r = wave; r < kZeroRows && first + r < A.vocab; r += kThreads / 64)
+            if (!(taken >> r & 1))
+                for (size_t c0 = 0; c0 < A.dim; c0 += L::kSlice) L::template finish<DW>((W *)A.d_weight + (first + r) * A.weight_stride, c0, A.dim, lane, zeros, 0.0f, false);
+        return;
+    }
+    const size_t item = (size_t)blockIdx.x * (kThreads / 64) + wave, piece = item / A.slices, c0 = item % A.slices * L::kSlice;
+    const size_t begin = piece * A.piece;
+    if (begin >= A.n) return;
+    const int count = (int)(begin + A.piece < A.n ? A.piece : A.n - begin);
+    // lane i: the piece's i-th pair; lane 62: the key in front, 63: the one behind (none there: one that no pair has)
+    const uint32_t none = 0xFFFFFFFFu;
+    uint32_t key = none, token = 0;
+    if (lane < count) { key = A.keys[begin + lane]; token = A.tokens[begin + lane]; }
+    if (lane == 62 && begin > 0) key = A.keys[begin - 1];
+    if (lane == 63 && begin + count < A.n) key = A.keys[begin + count];
+    const uint32_t before = (uint32_t)__builtin_amdgcn_readlane((int)key, 62), behind = (uint32_t)__builtin_amdgcn_readlane((int)key, 63);
+    float sum[L::N] = {};
+    bool from_before = (uint32_t)__builtin_amdgcn_readlane((int)key, 0) == before;
+    constexpr int kAhead = 8;
+    for (int i0 = 0; i0 < count; i0 += kAhead) {
+        typename L::Vec v[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (i0 + u < count) v[u] = L::load((const G *)A.d_out + (size_t)(uint32_t)__builtin_amdgcn_readlane((int)token, i0 + u) * A.out_stride, c0, A.dim, lane);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int i = i0 + u;
+            if (i >= count) break;
+            const uint32_t row = (uint32_t)__builtin_amdgcn_readlane((int)key, i);
+            L::add(sum, v[u]);
+            const bool ends = i + 1 == count || (uint32_t)__builtin_amdgcn_readlane((int)key, i + 1) != row;
+            if (!ends) continue;
+            const bool goes_on = i + 1 == count && behind == row;
+            if (row < A.vocab) {
+                if (from_before || goes_on) {
+                    float *p = A.partial + (2 * piece + (from_before ? 0 : 1)) * A.dim;
+#pragma unroll
+                    for (int k = 0; k < L::N; ++k)
+                        if (c0 + L::col(lane, k) < A.dim) p[c0 + L::col(lane, k)] = sum[k];
+                } else {
+                    L::template finish<DW>((W *)A.d_weight + (size_t)row * A.weight_stride, c0, A.dim, lane, sum, A.scale, A.accumulate);
+                }
+            }
+            from_before = false;
+#pragma unroll
+            for (int k = 0; k < L::N; ++k) sum[k] = 0.0f;
+        }
+    }
+}
+
+// The runs that lie in several pieces.  A workgroup looks at one piece and a slice of 64 columns: if a run starts in it and goes on behind it, its wavefronts
+// take the pieces that hold it in turns of consecutive ones, and the first of them adds the others' sums.
+constexpr int kJoinWaves = 8;
+template <int DW> __global__ __launch_bounds__(64 * kJoinWaves) void join_runs_kernel(GradArgs A)
+{
+    typedef typename Elem<DW>::T W;
+    const size_t piece = blockIdx.x, behind = (piece + 1) * A.piece;
+    if (behind >= A.n) return;
+    const uint32_t row = A.keys[behind];
+    if (A.keys[behind - 1] != row || row >= A.vocab) return;
+    if (piece > 0 && A.keys[piece * A.piece] == row && A.keys[piece * A.piece - 1] == row) return;      // (the run started before)
+    __shared__ size_t end;
+    __shared__ float sums[kJoinWaves][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (threadIdx.x == 0) {
+        size_t lo = behind, hi = A.n;              // the first pair behind the run
+        while (lo < hi) {
+            const size_t mid = lo + (hi - lo) / 2;
+            if (A.keys[mid] <= row) lo = mid + 1; else hi = mid;
+        }
+        end = (lo - 1) / A.piece + 1;              // the piece behind the run's last
+    }
+    __syncthreads();
+    const size_t count = end - piece, each = (count + kJoinWaves - 1) / kJoinWaves;
+    const size_t from = piece + wave * each, to = from + each < end ? from + each : end;
+    for (size_t c0 = 0; c0 < A.dim; c0 += 64) {
+        const size_t c = c0 + lane;
         float sum = 0.0f;
-        for (size_t p = lo; p < end; ++p) sum += (float)((const G *)A.d_out)[(size_t)A.tokens[p] * A.out_stride + i];
-        sum *= A.scale;
-        w[i] = (W)(A.accumulate ? (float)w[i] + sum : sum);
+        if (c < A.dim)
+            for (size_t p = from; p < to; ++p) sum += A.partial[(2 * p + (p == piece ? 1 : 0)) * A.dim + c];
+        sums[wave][lane] = sum;
+        __syncthreads();
+        if (wave == 0 && c < A.dim) {
+#pragma unroll
+            for (int w = 1; w < kJoinWaves; ++w) sum += sums[w][lane];
+            W *to_row = (W *)A.d_weight + (size_t)row * A.weight_stride;
+            to_row[c] = (W)(A.accumulate ? fmaf(sum, A.scale, (float)to_row[c]) : sum * A.scale);
+        }
+        __syncthreads();
     }
 }
 
@@ -100,28 +321,41 @@ template <template <int, int> class Pick> const void *pick(int a, int b)
 {
     return a == kF16 ? pick_second<Pick, kF16>(b) : a == kF32 ? pick_second<Pick, kF32>(b) : pick_second<Pick, kBF16>(b);
 }
-template <int W, int O> struct Lookup { static const void *fn() { return (const void *)lookup_kernel<W, O>; } };
-template <int G, int W> struct RowSums { static const void *fn() { return (const void *)row_sums_kernel<G, W>; } };
+constexpr int kTokensAtOnce = 4;
+template <int W, int O> struct Lookup { static const void *fn() { return (const void *)lookup_kernel<W, O, false, 1>; } };
+template <int W, int O> struct LookupAligned { static const void *fn() { return (const void *)lookup_kernel<W, O, true, 1>; } };
+template <int W, int O> struct LookupMany { static const void *fn() { return (const void *)lookup_kernel<W, O, false, kTokensAtOnce>; } };
+template <int W, int O> struct LookupManyAligned { static const void *fn() { return (const void *)lookup_kernel<W, O, true, kTokensAtOnce>; } };
+template <int G, int W> struct Few { static const void *fn() { return (const void *)few_tokens_kernel<G, W, false>; } };
+template <int G, int W> struct FewAligned { static const void *fn() { return (const void *)few_tokens_kernel<G, W, true>; } };
+template <int G, int W> struct Runs { static const void *fn() { return (const void *)sum_runs_kernel<G, W, false>; } };
+template <int G, int W> struct RunsAligned { static const void *fn() { return (const void *)sum_runs_kernel<G, W, true>; } };
+
+// Pairs to a piece.
+size_t piece_for(size_t) { return kMaxPiece; }
 
 // What the gradient's workspace holds, in bytes from its start.
 struct GradLayout {
-    size_t chain, keys, keys_tmp, tokens, tokens_tmp, flags, positions, all;
-    explicit GradLayout(size_t n)
+    size_t chain, keys, keys_tmp, tokens, tokens_tmp, flags, positions, partial, all;
+    GradLayout(size_t n, size_t dim)
     {
         const size_t words = (4 * n + 15) / 16 * 16;
         chain = tcuscan_workspace_bytes(1, n, TCUSCAN_I8_I32);          // what the sort asks for, in each of its forms
         if (chain < chain_layout::kHeaderBytes) chain = chain_layout::kHeaderBytes;
         keys = chain;
+        if (n <= kFewTokens) { keys_tmp = tokens = tokens_tmp = flags = positions = partial = all = chain; return; }
         keys_tmp = keys + words;
         tokens = keys_tmp + words;
         tokens_tmp = tokens + words;
         positions = tokens_tmp + words;
         flags = positions + words;
-        all = flags + (n + 15) / 16 * 16;
+        partial = flags + (n + 15) / 16 * 16;
+        all = partial + 2 * ((n + piece_for(n) - 1) / piece_for(n)) * dim * 4;
     }
 };
 
 constexpr size_t kMostRows = 0x7FFFFFFFu;
+constexpr size_t kManyItems = 1 << 14;      // wavefronts' items from which on each takes four tokens
 
 }  // namespace
 
@@ -138,16 +372,21 @@ tcuscan_status_t tcuscan_embedding(const void *d_ids, int id_bytes, size_t n, co
     if (!d_ids || !d_weight || !d_out || vocab == 0 || weight_stride < dim || out_stride < dim) return TCUSCAN_ERR_INVALID_ARG;
     if ((uintptr_t)d_ids % (size_t)id_bytes || (uintptr_t)d_weight % we || (uintptr_t)d_out % oe || d_out == d_weight) return TCUSCAN_ERR_INVALID_ARG;
     if (d_ws && (ws_bytes < chain_layout::kHeaderBytes || (uintptr_t)d_ws % 8)) return TCUSCAN_ERR_WORKSPACE;
-    const size_t blocks = (n + kThreads / 64 - 1) / (kThreads / 64);
+    const size_t cols = weight_dt == kF32 && out_dt == kF32 ? kLaneCols<kF32> : kLaneCols<kBF16>, slices = (dim + 64 * cols - 1) / (64 * cols);
+    const bool aligned = dim % cols == 0 && weight_stride % cols == 0 && out_stride % cols == 0 && (uintptr_t)d_weight % 16 == 0 && (uintptr_t)d_out % 16 == 0;
+    const bool many = n * slices >= kManyItems;
+    const size_t at_once = many ? kTokensAtOnce : 1, blocks = ((n + at_once - 1) / at_once * slices + kThreads / 64 - 1) / (kThreads / 64);
     if (blocks > kMostRows) return TCUSCAN_ERR_UNSUPPORTED;
-    LookupArgs A = {d_ids, d_weight, d_out, d_ws, n, vocab, dim, weight_stride, out_stride, scale, id_bytes == 8};
+    LookupArgs A = {d_ids, d_weight, d_out, d_ws, n, vocab, dim, weight_stride, out_stride, slices, scale, id_bytes == 8};
     void *args[] = {&A};
-    return hipLaunchKernel(pick<Lookup>(weight_dt, out_dt), dim3((unsigned)blocks), dim3(kThreads), args, 0, (hipStream_t)stream) == hipSuccess ? TCUSCAN_OK : TCUSCAN_ERR_HIP;
+    const void *fn = many ? aligned ? pick<LookupManyAligned>(weight_dt, out_dt) : pick<LookupMany>(weight_dt, out_dt)
+                          : aligned ? pick<LookupAligned>(weight_dt, out_dt) : pick<Lookup>(weight_dt, out_dt);
+    return hipLaunchKernel(fn, dim3((unsigned)blocks), dim3(kThreads), args, 0, (hipStream_t)stream) == hipSuccess ? TCUSCAN_OK : TCUSCAN_ERR_HIP;
 }
 
 size_t tcuscan_embedding_backward_workspace_bytes(size_t n, size_t vocab, size_t dim)
 {
-    return n > 0xFFFFFFFFull || vocab == 0 || vocab > kMostRows || dim == 0 ? 0 : GradLayout(n).all;
+    return n > 0xFFFFFFFFull || vocab == 0 || vocab > kMostRows || dim == 0 ? 0 : GradLayout(n, dim).all;
 }
 
 tcuscan_status_t tcuscan_embedding_backward(const void *d_ids, int id_bytes, size_t n, const void *d_out_grad, size_t out_stride, tcuscan_dtype_t out_dt,
@@ -162,22 +401,40 @@ tcuscan_status_t tcuscan_embedding_backward(const void *d_ids, int id_bytes, siz
     if (!d_weight_grad || weight_stride < dim || (uintptr_t)d_weight_grad % we) return TCUSCAN_ERR_INVALID_ARG;
     if (n && (!d_ids || !d_out_grad || out_stride < dim || d_out_grad == d_weight_grad)) return TCUSCAN_ERR_INVALID_ARG;
     if ((uintptr_t)d_ids % (size_t)id_bytes || (uintptr_t)d_out_grad % oe) return TCUSCAN_ERR_INVALID_ARG;
-    const GradLayout L(n);
+    const GradLayout L(n, dim);
     if (!d_ws || ws_bytes < L.all || (uintptr_t)d_ws % 16) return TCUSCAN_ERR_WORKSPACE;
     char *ws = (char *)d_ws;
     hipStream_t s = (hipStream_t)stream;
-    GradArgs A = {d_ids, d_out_grad, d_weight_grad, d_ws, (uint32_t *)(ws + L.keys), (uint32_t *)(ws + L.tokens),
-                  n, vocab, dim, out_stride, weight_stride, padding, scale, id_bytes == 8, accumulate};
+    GradArgs A = {};
+    A.ids = d_ids; A.d_out = d_out_grad; A.d_weight = d_weight_grad; A.ws = d_ws;
+    A.keys = (uint32_t *)(ws + L.keys); A.tokens = (uint32_t *)(ws + L.tokens); A.partial = (float *)(ws + L.partial);
+    A.n = n; A.vocab = vocab; A.dim = dim; A.out_stride = out_stride; A.weight_stride = weight_stride;
+    A.padding = padding; A.scale = scale; A.wide_ids = id_bytes == 8; A.accumulate = accumulate;
     void *args[] = {&A};
-    if (n) {
-        if (hipLaunchKernel((const void *)token_keys_kernel, dim3((unsigned)((n + kThreads - 1) / kThreads)), dim3(kThreads), args, 0, s) != hipSuccess) return TCUSCAN_ERR_HIP;
-        int bits = 0;
-        while (((size_t)1 << bits) <= vocab) ++bits;
-        const tcuscan_status_t st = tcuscan_split_radix_sort_u32(A.keys, A.tokens, n, bits, ws + L.keys_tmp, ws + L.tokens_tmp, ws + L.flags, ws + L.positions,
-                                                                 d_ws, L.chain, stream);
-        if (st != TCUSCAN_OK) return st;
+    const size_t cols = out_dt == kF32 ? kLaneCols<kF32> : kLaneCols<kBF16>;
+    const bool aligned = dim % cols == 0 && out_stride % cols == 0 && weight_stride % cols == 0 && (uintptr_t)d_out_grad % 16 == 0 && (uintptr_t)d_weight_grad % (cols * we) == 0;
+    if (n <= kFewTokens) {
+        // as many workgroups as keep the chip busy, and no more than that: each of them reads all token numbers
+        A.rows = 4;
+        while (A.rows < kMaxFewRows && vocab / A.rows > 1024) A.rows *= 2;
+        const void *fn = aligned ? pick<FewAligned>(out_dt, weight_dt) : pick<Few>(out_dt, weight_dt);
+        return hipLaunchKernel(fn, dim3((unsigned)((vocab + A.rows - 1) / A.rows)), dim3(kThreads), args, 0, s) == hipSuccess ? TCUSCAN_OK : TCUSCAN_ERR_HIP;
     }
-    return hipLaunchKernel(pick<RowSums>(out_dt, weight_dt), dim3((unsigned)vocab), dim3(kThreads), args, 0, s) == hipSuccess ? TCUSCAN_OK : TCUSCAN_ERR_HIP;
+    if (hipLaunchKernel((const void *)token_keys_kernel, dim3((unsigned)((n + kThreads - 1) / kThreads)), dim3(kThreads), args, 0, s) != hipSuccess) return TCUSCAN_ERR_HIP;
+    int bits = 0;
+    while (((size_t)1 << bits) <= vocab) ++bits;
+    const tcuscan_status_t st = tcuscan_split_radix_sort_u32(A.keys, A.tokens, n, bits, ws + L.keys_tmp, ws + L.tokens_tmp, ws + L.flags, ws + L.positions,
+                                                             d_ws, L.chain, stream);
+    if (st != TCUSCAN_OK) return st;
+    A.piece = piece_for(n);
+    A.slices = (dim + 64 * cols - 1) / (64 * cols);
+    const size_t pieces = (n + A.piece - 1) / A.piece, zero_groups = accumulate ? 0 : (vocab + kZeroRows - 1) / kZeroRows;
+    A.piece_groups = (pieces * A.slices + kThreads / 64 - 1) / (kThreads / 64);
+    if (A.piece_groups + zero_groups > kMostRows) return TCUSCAN_ERR_UNSUPPORTED;
+    const void *fn = aligned ? pick<RunsAligned>(out_dt, weight_dt) : pick<Runs>(out_dt, weight_dt);
+    if (hipLaunchKernel(fn, dim3((unsigned)(A.piece_groups + zero_groups)), dim3(kThreads), args, 0, s) != hipSuccess) return TCUSCAN_ERR_HIP;
+    fn = weight_dt == kF16 ? (const void *)join_runs_kernel<kF16> : weight_dt == kF32 ? (const void *)join_runs_kernel<kF32> : (const void *)join_runs_kernel<kBF16>;
+    return hipLaunchKernel(fn, dim3((unsigned)pieces), dim3(64 * kJoinWaves), args, 0, s) == hipSuccess ? TCUSCAN_OK : TCUSCAN_ERR_HIP;
 }
 
 }  // extern "C"
