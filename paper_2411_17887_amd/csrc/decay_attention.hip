@@ -49,8 +49,6 @@ struct WalkArgs {
     float by_new, by_read;
     int from_end;
     int wide;                                      // the output is fp32 whatever the element type
-    int whole;                                     // bits 0 to 2: eight elements of x, y, z are aligned 16-byte granules (two for fp32) and
-                                                   // all inside or all outside; bit 3: four elements of the output likewise
 };
 
 // a^n, for weights.  (An n of 0 gives 1 for a decay of 0, a log_decay of minus infinity, too.)
@@ -58,14 +56,15 @@ __device__ __forceinline__ float decay_power(float log_decay, float n) { return 
 // Takes a state n tokens on: m becomes a^n m.  Slow decays (a^n from 1/2 on) as m + (a^n - 1) m: multiplied by a rounded a^n, a state
 // would be off by up to half a unit in the last place of 1 each time, always to the same side: 1e-5 for 1 - 2^-9 token by token.
 struct Decay {
-    float by, keep;
+    float by;
+    bool slow;
     __device__ __forceinline__ Decay(float log_decay, float n)
     {
         const float x = fmaxf(log_decay, -1e30f) * n;
-        keep = x > -0.69f ? 1.0f : 0.0f;
-        by = x > -0.69f ? expm1f(x) : __expf(x);
+        slow = x > -0.69f;
+        by = slow ? expm1f(x) : __expf(x);
     }
-    __device__ __forceinline__ float operator()(float m) const { return fmaf(m, by, keep * m); }
+    __device__ __forceinline__ float operator()(float m) const { return fmaf(m, by, slow ? m : 0.0f); }
 };
 
 // Row r's tokens, clipped to the arrays.
@@ -91,7 +90,7 @@ __device__ __forceinline__ long long state_of(const long long *slots, unsigned r
 //   M    <- a^C M + sum over j of by_new a^(C-1-j) y_j^T z_j                          (from the end a^(C-j))
 //
 // Every sum over features or tokens is a matrix product: P^T = Y X^T (then weighted and cut to j <= i), out^T = M^T X^T and Z^T P^T,
-// M += Y^T (wZ).  A wavefront owns 16 columns of Z, out and M and all A rows of M, in MFMA accumulators from the first token to the
+// M += Y^T (wZ).  A wavefront owns 16 CT columns of Z, out and M and all A rows of M, in MFMA accumulators from the first token to the
 // last.  The products are ordered so that operands fall into the lanes that have them: the accumulators of M, two row tiles side by side, are
 // the left operand of M^T X^T as they stand (tile rows are dealt so that a lane's eight values are eight consecutive a), and Z's columns are
 // read transposed once, for Z^T P^T and, weighted, for the update.  Only X, Y, Z (shared by all wavefronts of the workgroup) and P go through LDS.
@@ -107,22 +106,30 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short  s16x4 __attribute__((ext_vector_type(4)));
 typedef short  s16x8 __attribute__((ext_vector_type(8)));
 typedef float  f32x4 __attribute__((ext_vector_type(4)));
+typedef float  f32x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int parts_of(int dt) { return dt == kBF16 ? 1 : dt == kF16 ? 2 : 3; }
 // Tokens of a block: what LDS holds of X, Y and Z next to each other.
 constexpr int block_tokens(int dt, int ap) { return dt == kF32 || (dt == kF16 && ap > 128) ? 32 : 64; }
 
+constexpr int kWalkWaves = 4;
+// Workgroups on a compute unit, by what LDS and registers give.
+constexpr int groups_at_once(int dt, int ap, int ct) { return ap > 128 || (dt != kBF16 && ap > 64) || (dt == kF16 && ct > 1) ? 1 : 2; }
+
 template <int N> struct Parts { bf16x8 p[N]; };
 
-// The first N bf16 parts of x: x = part 0 + part 1 + ..., each the rounding of what the ones before leave.
-template <int N> __device__ __forceinline__ void split(float x, bf16_t (&p)[N])
+// The first N bf16 parts of eight values: x = part 0 + part 1 + ..., each the rounding of what the ones before leave.
+template <int N> __device__ __forceinline__ Parts<N> split(f32x8 x)
 {
+    Parts<N> parts;
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-        p[n] = (bf16_t)x;
-        x -= (float)p[n];
+        parts.p[n] = __builtin_convertvector(x, bf16x8);
+        x -= __builtin_convertvector(parts.p[n], f32x8);
     }
+    return parts;
 }
 // acc += a b for sums of parts: all products a[i] b[j] with i + j < kOrder.
 template <int kOrder, int NA, int NB> __device__ __forceinline__ f32x4 product(const Parts<NA> &a, const Parts<NB> &b, f32x4 acc)
@@ -149,79 +156,101 @@ template <int COLS> struct Tile {
     __device__ __forceinline__ static int at(int row, int col) { return row * COLS + ((((col >> 3) ^ swizzle(row)) << 3) | (col & 7)); }
 };
 
-// Reads the transposed operand: lane l of group g receives tile[row][column of lane l] for the eight rows row0 + 8 g .. + 7.  The
-// instruction hands lane l of 16 the l-th column of the four rows whose 16 pieces of four columns the 16 lanes point at: lane s at row s / 4, piece
-// s % 4, which starts at column col0 + piece * (s % 4).
+// Where a lane finds operands.  Both kinds of reading go through one number per lane and tile shape; the operand's place in the tile then is an exclusive or
+// with a constant (columns) and a constant offset (rows, which the swizzle repeats every 16 of).
+//
+// Row operand: lane l of group g receives the eight columns k0 + 8 g .. + 7 of row row0 + l (row0 a multiple of 16, k0 of 32).
+template <int COLS> __device__ __forceinline__ int row_lane(int lane) { return Tile<COLS>::at(lane & 15, 8 * (lane >> 4)); }
+template <int COLS> __device__ __forceinline__ bf16x8 row_operand(const bf16_t *tile, int mine, int row0, int k0) { return *(const bf16x8 *)(tile + row0 * COLS + (mine ^ k0)); }
+// Column operand: lane l of group g receives one column of the eight rows row0 + 8 g .. + 7 (row0 a multiple of 32).  The instruction hands lane l of 16 the
+// l-th column of the four rows whose 16 pieces of four columns the 16 lanes point at: lane s at row s / 4 and piece s % 4, which starts PIECE columns behind the
+// one before.  `first`: the wavefront's first column, a multiple of 32 (of 16, if it is the only one); col0: from there, a multiple of 16 or with PIECE = 8
+// of 32, and there + 4 for the other halves of the pieces' granules.
 __device__ __forceinline__ s16x4 read_transposed(const bf16_t *p)
 {
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)p);
 }
-template <int COLS> __device__ __forceinline__ bf16x8 column_operand(const bf16_t *tile, int row0, int col0, int piece, int lane)
+template <int COLS, int PIECE> __device__ __forceinline__ int column_lane(int lane, int first) { return Tile<COLS>::at(8 * (lane >> 4) + ((lane & 15) >> 2), first + PIECE * (lane & 3)); }
+template <int COLS> __device__ __forceinline__ bf16x8 column_operand(const bf16_t *tile, int mine, int row0, int col0)
 {
-    const int row = row0 + 8 * (lane >> 4) + ((lane & 15) >> 2), col = col0 + piece * (lane & 3);
-    const s16x4 a = read_transposed(tile + Tile<COLS>::at(row, col)), b = read_transposed(tile + Tile<COLS>::at(row + 4, col));
+    const bf16_t *p = tile + row0 * COLS + (col0 & 4);
+    const int at = mine ^ (col0 & ~4);             // four rows on, the swizzle differs in its lowest bit
+    const s16x4 a = read_transposed(p + at), b = read_transposed(p + 4 * COLS + (at ^ 8));
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
-// Lane l of group g receives the eight columns k0 + 8 g .. + 7 of row row0 + l.
-template <int COLS> __device__ __forceinline__ bf16x8 row_operand(const bf16_t *tile, int row0, int k0, int lane)
+// Keeps the compiler from computing what depends on v ahead of a loop: addresses made of a lane's number and constants would take dozens of registers.
+__device__ __forceinline__ int here(int v)
 {
-    return *(const bf16x8 *)(tile + Tile<COLS>::at(row0 + (lane & 15), k0 + 8 * (lane >> 4)));
+    asm volatile("" : "+v"(v));
+    return v;
 }
 
-// A block of tokens on its way from memory to LDS: C rows of COLS elements, eight at a time, spread over THREADS lanes.
-template <int DT, int C, int COLS, int THREADS> struct Stage {
+// A block of tokens on its way from memory to LDS: C rows of COLS elements, eight at a time, spread over THREADS lanes.  WHOLE: granules of eight
+// elements are aligned and either inside or outside; they wait in registers while the block before is worked on.  Otherwise the block is
+// read element by element when its turn comes.
+template <int DT, int C, int COLS, int THREADS, bool WHOLE> struct Stage {
     typedef typename Elem<DT>::T T;
-    static constexpr int kItems = C * COLS / 8, kEach = (kItems + THREADS - 1) / THREADS, kQuads = sizeof(T) / 2;
-    u32x4 v[kEach][kQuads];
+    static constexpr int kItems = C * COLS / 8, kEach = (kItems + THREADS - 1) / THREADS, kQuads = sizeof(T) / 2, N = parts_of(DT);
+    static constexpr int kRowsAtOnce = THREADS / (COLS / 8);
+    static_assert(THREADS % (COLS / 8) == 0, "a lane keeps to its columns");
+    u32x4 v[WHOLE ? kEach : 1][kQuads];
+    const T *mine;                                 // the lane's first granule in the block
+    long long step;                                // from row to row
+    int row, col, cols;
 
-    // Row i of the block is at p + i * step; rows from n on and columns from `cols` on are zeros.  `whole`: granules of eight elements are
-    // aligned and either inside or outside.
-    __device__ __forceinline__ void load(const T *p, long long step, int n, int cols, bool whole)
+    __device__ __forceinline__ void begin(const T *p, long long row_step, int columns)
     {
+        row = (int)threadIdx.x / (COLS / 8); col = (int)threadIdx.x % (COLS / 8) * 8; cols = columns; step = row_step;
+        mine = p + row * step + col;
+    }
+    // Rows from n on and columns from `cols` on are zeros.
+    __device__ __forceinline__ void load(int n)
+    {
+        if constexpr (!WHOLE) return;
+        const T *p = mine;
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int item = i * THREADS + (int)threadIdx.x, row = item / (COLS / 8), col = item % (COLS / 8) * 8;
-            const bool there = item < kItems && row < n && col < cols;
+        for (int i = 0; i < kEach; ++i, p += kRowsAtOnce * step) {
 #pragma unroll
             for (int q = 0; q < kQuads; ++q) v[i][q] = u32x4{0u, 0u, 0u, 0u};
-            if (!there) continue;
-            const T *src = p + row * step + col;
-            if (whole) {
+            if (row + i * kRowsAtOnce < n && col < cols)
 #pragma unroll
-                for (int q = 0; q < kQuads; ++q) v[i][q] = ((const u32x4 *)src)[q];
-            } else {
-                T e[8];
-#pragma unroll
-                for (int k = 0; k < 8; ++k) e[k] = col + k < cols ? src[k] : (T)0.0f;
-                __builtin_memcpy(&v[i][0], e, sizeof e);
-            }
+                for (int q = 0; q < kQuads; ++q) v[i][q] = ((const u32x4 *)p)[q];
         }
     }
-    __device__ __forceinline__ void store(bf16_t *tile) const                     // the parts are C * COLS elements apart
+    static __device__ __forceinline__ void put(bf16_t *to, const T (&e)[8])                       // the parts are C * COLS elements apart
     {
-        constexpr int N = parts_of(DT);
+        if constexpr (N == 1) {
+            __builtin_memcpy(to, e, 16);
+        } else {
+            f32x8 x;
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int item = i * THREADS + (int)threadIdx.x, row = item / (COLS / 8), col = item % (COLS / 8) * 8;
-            if (item >= kItems) break;
-            bf16_t *to = tile + Tile<COLS>::at(row, col);
-            if constexpr (N == 1) {
-                *(u32x4 *)to = v[i][0];
-            } else {
+            for (int k = 0; k < 8; ++k) x[k] = (float)e[k];
+            const Parts<N> parts = split<N>(x);
+#pragma unroll
+            for (int n = 0; n < N; ++n) *(bf16x8 *)(to + n * C * COLS) = parts.p[n];
+        }
+    }
+    // (and on to the next block)
+    __device__ __forceinline__ void store(bf16_t *tile, int n)
+    {
+        if constexpr (WHOLE) {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
                 T e[8];
                 __builtin_memcpy(e, &v[i][0], sizeof e);
-                bf16x8 part[N];
+                if (row + i * kRowsAtOnce < C) put(tile + Tile<COLS>::at(row + i * kRowsAtOnce, col), e);
+            }
+        } else {
+#pragma unroll 1
+            for (int r = row; r < C; r += kRowsAtOnce) {
+                const T *p = mine + (r - row) * step;
+                T e[8];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    bf16_t p[N];
-                    split<N>((float)e[k], p);
-#pragma unroll
-                    for (int n = 0; n < N; ++n) part[n][k] = p[n];
-                }
-#pragma unroll
-                for (int n = 0; n < N; ++n) *(bf16x8 *)(to + n * C * COLS) = part[n];
+                for (int k = 0; k < 8; ++k) e[k] = r < n && col + k < cols ? p[k] : (T)0.0f;
+                put(tile + Tile<COLS>::at(r, col), e);
             }
         }
+        mine += C * step;
     }
 };
 
@@ -255,23 +284,45 @@ __device__ __forceinline__ bool find_piece(const WalkArgs &W, unsigned number, P
     return true;
 }
 
-// Four consecutive columns of the output.  `whole`: they are aligned and all inside or all outside.
-template <class T> __device__ __forceinline__ void store_four(T *row, int col, int cols, f32x4 v, float by, bool whole)
+// Four consecutive columns of the output, `col` the first of them.  WHOLE: they are aligned and all inside or all outside.
+template <class T, bool WHOLE> __device__ __forceinline__ void store_four(T *p, int col, int cols, f32x4 v)
 {
     typedef T T4 __attribute__((ext_vector_type(4)));
-    if (whole) {
-        if (col < cols) *(T4 *)(row + col) = T4{(T)(v[0] * by), (T)(v[1] * by), (T)(v[2] * by), (T)(v[3] * by)};
+    if constexpr (WHOLE) {
+        if (col < cols) *(T4 *)p = __builtin_convertvector(v, T4);
     } else {
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-            if (col + r < cols) row[col + r] = (T)(v[r] * by);
+            if (col + r < cols) p[r] = (T)v[r];
     }
 }
 
-template <int DT, int AP, int WAVES> __global__ __launch_bounds__(64 * WAVES) void walk_kernel(WalkArgs W)
+// Calls what(element, its index) for the lane's elements of a state that exist.  The lane's number passes through an empty asm statement: otherwise
+// the compiler keeps every element's address and predicate from the reading of a state to its writing, registers that the walk needs.
+template <int AP, int CT, class What> __device__ __forceinline__ void each_of_state(f32x4 (&M)[AP / 16][CT], bool any, unsigned first_e, unsigned A, unsigned E, size_t m_a,
+                                                                                    size_t m_e, What what)
+{
+    unsigned lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    if (!any) return;
+    const unsigned a0 = 8 * (lane >> 4), e_lane = first_e + (lane & 15);
+#pragma unroll
+    for (int t = 0; t < AP / 16; ++t)
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const unsigned a = a0 + 32 * (t / 2) + 4 * (t & 1) + r, e = e_lane + 16 * c;
+                float m = M[t][c][r];
+                if (a < A && e < E) what(m, a * m_a + e * m_e);
+                M[t][c][r] = m;
+            }
+}
+
+template <int DT, int AP, int CT, bool WHOLE> __global__ __launch_bounds__(64 * kWalkWaves, groups_at_once(DT, AP, CT)) void walk_kernel(WalkArgs W)
 {
     typedef typename Elem<DT>::T T;
-    constexpr int N = parts_of(DT), C = block_tokens(DT, AP), EB = 16 * WAVES, kThreads = 64 * WAVES;
+    constexpr int N = parts_of(DT), C = block_tokens(DT, AP), EB = 16 * kWalkWaves * CT, kThreads = 64 * kWalkWaves;
     constexpr int kTiles = C / 16, kSteps = C / 32, kOrder = N == 3 ? 3 : 2;       // tiles of 16 tokens, steps of 32
     __shared__ __attribute__((aligned(16))) bf16_t sx[N * C * AP], sy[N * C * AP], sz[N * C * EB], sp[N * C * C];
     __shared__ __attribute__((aligned(16))) float weight[C];
@@ -291,25 +342,17 @@ template <int DT, int AP, int WAVES> __global__ __launch_bounds__(64 * WAVES) vo
     if (!reads && piece.last) return;              // (what a row's last segment adds, nobody asks for)
 
     const float log_decay = W.log_decay[h];
-    const int e0 = (int)block * EB;                // the workgroup's first column
-    const unsigned e = e0 + 16 * wave + l;         // the lane's
-    const bool column = e < W.E;
+    const int e0 = (int)block * EB, wave_e = 16 * CT * wave;        // the workgroup's first column, and the wavefront's of these
     const long long slot = state_of(W.slots, piece.r, W.states);
     const size_t state = ((size_t)slot * W.heads + h) * W.A * W.E, between = ((size_t)number * W.heads + h) * W.A * W.E;
-
-    // M[2 s + t][r] is M[a][e] with a = 32 s + 8 g + 4 t + r
-    f32x4 M[AP / 16];
+    const bool cut = piece.first > 0 || !piece.last;                // a row of several segments
+    // M[2 s + t][c][r] is M[a][e] with a = 32 s + 8 g + 4 t + r, e = e0 + wave_e + 16 c + l
+    f32x4 M[AP / 16][CT] = {};
     {
         // a row of several segments finds what it starts from in the workspace, also for the first of them
-        const float *from = !reads ? nullptr : piece.first > 0 || !piece.last ? W.between + between : W.m_in && slot >= 0 ? W.m_in + state : nullptr;
-        const bool own = reads && (piece.first > 0 || !piece.last);
-#pragma unroll
-        for (int t = 0; t < AP / 16; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const unsigned a = 32 * (t / 2) + 8 * g + 4 * (t & 1) + r;
-                M[t][r] = from && column && a < W.A ? from[own ? (size_t)a * W.E + e : (size_t)a * W.m_a + (size_t)e * W.m_e] : 0.0f;
-            }
+        const float *from = !reads ? nullptr : cut ? W.between + between : W.m_in && slot >= 0 ? W.m_in + state : nullptr;
+        const size_t m_a = cut ? W.E : W.m_a, m_e = cut ? 1 : W.m_e;
+        each_of_state<AP, CT>(M, from != nullptr, e0 + wave_e, W.A, W.E, m_a, m_e, [&](float &m, size_t i) { m = from[i]; });
     }
     float reading[kTiles];                         // a^(i+1), from the end a^i, of the lane's token in each tile
 #pragma unroll
@@ -320,34 +363,38 @@ template <int DT, int AP, int WAVES> __global__ __launch_bounds__(64 * WAVES) vo
             *(u32x4 *)(sp + n * C * C + Tile<C>::at(32 * t + row, 32 * t + 16 + 8 * half)) = u32x4{0u, 0u, 0u, 0u};
         }
 
-    const long long sign = W.from_end ? -1 : 1, origin = W.from_end ? piece.hi - 1 : piece.lo;
-    const T *x = (const T *)W.x.data + W.x.at(h, W.heads), *y = (const T *)W.y.data + W.y.at(h, W.heads), *z = (const T *)W.z.data + W.z.at(h, W.heads) + e0;
-    const int ecols = (int)W.E - e0;
-    Stage<DT, C, AP, kThreads> next_x, next_y;
-    Stage<DT, C, EB, kThreads> next_z;
-    auto fetch = [&](long long at) {
-        const int n = (int)(piece.end - at < C ? piece.end - at : C);
-        const long long t = origin + sign * at;
-        if (reads) next_x.load(x + t * W.x.token, sign * W.x.token, n, (int)W.A, W.whole & 1);
-        next_y.load(y + t * W.y.token, sign * W.y.token, n, (int)W.A, W.whole & 2);
-        next_z.load(z + t * W.z.token, sign * W.z.token, n, ecols, W.whole & 4);
+    const long long sign = W.from_end ? -1 : 1, origin = (W.from_end ? piece.hi - 1 : piece.lo) + sign * piece.first;
+    Stage<DT, C, AP, kThreads, WHOLE> next_x, next_y;
+    Stage<DT, C, EB, kThreads, WHOLE> next_z;
+    next_x.begin((const T *)W.x.data + W.x.at(h, W.heads) + origin * W.x.token, sign * W.x.token, (int)W.A);
+    next_y.begin((const T *)W.y.data + W.y.at(h, W.heads) + origin * W.y.token, sign * W.y.token, (int)W.A);
+    next_z.begin((const T *)W.z.data + W.z.at(h, W.heads) + origin * W.z.token + e0, sign * W.z.token, (int)W.E - e0);
+    // the lane's first output: token l of the block, column 4 g of the wavefront's
+    const int out_size = W.wide ? 4 : (int)sizeof(T);
+    char *out = (char *)W.out.data + (W.out.at(h, W.heads) + (origin + sign * l) * W.out.token + e0 + wave_e + 4 * g) * out_size;
+    const long long out_step = sign * 16 * W.out.token * out_size;
+    const long long length = piece.end - piece.first;
+    auto fetch = [&](long long left) {
+        const int n = (int)(left < C ? left : C);
+        if (reads) next_x.load(n);
+        next_y.load(n);
+        next_z.load(n);
     };
-    if (piece.first < piece.end) fetch(piece.first);
-    for (long long at = piece.first; at < piece.end; at += C) {
-        const int n = (int)(piece.end - at < C ? piece.end - at : C);
-        if (reads) next_x.store(sx);
-        next_y.store(sy);
-        next_z.store(sz);
+    if (length > 0) fetch(length);
+    for (long long at = 0; at < length; at += C) {
+        const int n = (int)(length - at < C ? length - at : C);
+        const int row_at = here(row_lane<AP>(lane)), p_at = here(row_lane<C>(lane)), y_at = here(column_lane<AP, 8>(lane, 0)), z_at = here(column_lane<EB, 4>(lane, wave_e));
+        if (reads) next_x.store(sx, n);
+        next_y.store(sy, n);
+        next_z.store(sz, n);
         if ((int)threadIdx.x < C)
             weight[threadIdx.x] = (int)threadIdx.x < n ? W.by_new * decay_power(log_decay, (float)(n - 1 - (int)threadIdx.x + (W.from_end ? 1 : 0))) : 0.0f;
         __syncthreads();
-        if (at + C < piece.end) fetch(at + C);
-
         if (reads) {
             // P^T, 16 keys by 16 queries at a time
 #pragma unroll
-            for (int k = 0; k < (kTiles * (kTiles + 1) / 2 + WAVES - 1) / WAVES; ++k) {
-                const int tile = wave + k * WAVES;
+            for (int k = 0; k < (kTiles * (kTiles + 1) / 2 + kWalkWaves - 1) / kWalkWaves; ++k) {
+                const int tile = wave + k * kWalkWaves;
                 if (tile >= kTiles * (kTiles + 1) / 2) break;
                 const int it = tile >= 6 ? 3 : tile >= 3 ? 2 : tile >= 1 ? 1 : 0, jt = tile - it * (it + 1) / 2;
                 f32x4 p = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -356,110 +403,117 @@ template <int DT, int AP, int WAVES> __global__ __launch_bounds__(64 * WAVES) vo
                     Parts<N> a, b;
 #pragma unroll
                     for (int m = 0; m < N; ++m) {
-                        a.p[m] = row_operand<AP>(sy + m * C * AP, 16 * jt, 32 * s, lane);
-                        b.p[m] = row_operand<AP>(sx + m * C * AP, 16 * it, 32 * s, lane);
+                        a.p[m] = row_operand<AP>(sy + m * C * AP, row_at, 16 * jt, 32 * s);
+                        b.p[m] = row_operand<AP>(sx + m * C * AP, row_at, 16 * it, 32 * s);
                     }
                     p = product<kOrder>(a, b, p);
                 }
                 const int i = 16 * it + l, j = 16 * jt + 4 * g;
-                bf16_t parts[4][N];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) split<N>(j + r <= i ? p[r] * (W.by_new * decay_power(log_decay, (float)(i - j - r))) : 0.0f, parts[r]);
+                for (int r = 0; r < 4; ++r) p[r] = j + r <= i ? p[r] * (W.by_new * decay_power(log_decay, (float)(i - j - r))) : 0.0f;
 #pragma unroll
                 for (int m = 0; m < N; ++m) {
-                    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-                    *(bf16x4 *)(sp + m * C * C + Tile<C>::at(i, j)) = bf16x4{parts[0][m], parts[1][m], parts[2][m], parts[3][m]};
+                    const bf16x4 part = __builtin_convertvector(p, bf16x4);
+                    *(bf16x4 *)(sp + m * C * C + Tile<C>::at(i, j)) = part;
+                    p -= __builtin_convertvector(part, f32x4);
                 }
             }
             __syncthreads();
         }
-        Parts<N> zt[kSteps];                       // 16 columns of Z by 32 tokens
+        Parts<N> zt[kSteps][CT];                   // 16 columns of Z by 32 tokens
 #pragma unroll
         for (int s = 0; s < kSteps; ++s)
 #pragma unroll
-            for (int m = 0; m < N; ++m) zt[s].p[m] = column_operand<EB>(sz + m * C * EB, 32 * s, 16 * wave, 4, lane);
+            for (int c = 0; c < CT; ++c)
+#pragma unroll
+                for (int m = 0; m < N; ++m) zt[s][c].p[m] = column_operand<EB>(sz + m * C * EB, z_at, 32 * s, 16 * c);
         if (reads) {
             constexpr int NM = N == 3 ? 3 : 2;
-            f32x4 o[kTiles];
+            f32x4 o[kTiles][CT];
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t) o[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                for (int c = 0; c < CT; ++c) o[t][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int s = 0; s < AP / 32; ++s) {
-                Parts<NM> m;
+                __builtin_amdgcn_sched_barrier(0);             // (or the parts of all steps take registers at once)
+                Parts<NM> m[CT];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    bf16_t part[NM];
-                    split<NM>(M[2 * s + k / 4][k % 4], part);
-#pragma unroll
-                    for (int i = 0; i < NM; ++i) m.p[i][k] = part[i];
-                }
+                for (int c = 0; c < CT; ++c) m[c] = split<NM>(__builtin_shufflevector(M[2 * s][c], M[2 * s + 1][c], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
                 for (int t = 0; t < kTiles; ++t) {
                     Parts<N> b;
 #pragma unroll
-                    for (int i = 0; i < N; ++i) b.p[i] = row_operand<AP>(sx + i * C * AP, 16 * t, 32 * s, lane);
-                    o[t] = product<kOrder>(m, b, o[t]);
+                    for (int i = 0; i < N; ++i) b.p[i] = row_operand<AP>(sx + i * C * AP, row_at, 16 * t, 32 * s);
+#pragma unroll
+                    for (int c = 0; c < CT; ++c) o[t][c] = product<kOrder>(m[c], b, o[t][c]);
                 }
             }
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r) o[t][r] *= reading[t];
+                for (int c = 0; c < CT; ++c) o[t][c] *= reading[t];
 #pragma unroll
                 for (int s = 0; s <= t / 2; ++s) {
                     Parts<N> b;
 #pragma unroll
-                    for (int i = 0; i < N; ++i) b.p[i] = row_operand<C>(sp + i * C * C, 16 * t, 32 * s, lane);
-                    o[t] = product<kOrder>(zt[s], b, o[t]);
+                    for (int i = 0; i < N; ++i) b.p[i] = row_operand<C>(sp + i * C * C, p_at, 16 * t, 32 * s);
+#pragma unroll
+                    for (int c = 0; c < CT; ++c) o[t][c] = product<kOrder>(zt[s][c], b, o[t][c]);
                 }
             }
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t) {
+            for (int t = 0; t < kTiles; ++t, out += out_step) {
                 if (16 * t + l >= n) continue;
-                const long long token = origin + sign * (at + 16 * t + l);
-                const int col = e0 + 16 * wave + 4 * g;
-                if (W.wide) store_four((float *)W.out.data + W.out.at(h, W.heads) + token * W.out.token, col, (int)W.E, o[t], W.by_read, W.whole & 8);
-                else store_four((T *)W.out.data + W.out.at(h, W.heads) + token * W.out.token, col, (int)W.E, o[t], W.by_read, W.whole & 8);
+#pragma unroll
+                for (int c = 0; c < CT; ++c) {
+                    const int col = e0 + wave_e + 16 * c + 4 * g;
+                    const f32x4 v = o[t][c] * W.by_read;
+                    if (W.wide) store_four<float, WHOLE>((float *)out + 16 * c, col, (int)W.E, v);
+                    else store_four<T, WHOLE>((T *)out + 16 * c, col, (int)W.E, v);
+                }
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
+        if (at + C < length) fetch(length - at - C);
         // the state
         const Decay decay(log_decay, (float)n);
+        if (decay.slow)
 #pragma unroll
-        for (int t = 0; t < AP / 16; ++t)
+            for (int t = 0; t < AP / 16; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) M[t][r] = decay(M[t][r]);
+                for (int c = 0; c < CT; ++c) M[t][c] = __builtin_elementwise_fma(M[t][c], f32x4{decay.by, decay.by, decay.by, decay.by}, M[t][c]);
+        else
+#pragma unroll
+            for (int t = 0; t < AP / 16; ++t)
+#pragma unroll
+                for (int c = 0; c < CT; ++c) M[t][c] *= decay.by;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
-            Parts<3> wz;
+            __builtin_amdgcn_sched_barrier(0);
+            const f32x8 w = *(const f32x8 *)(weight + 32 * s + 8 * g);
+            Parts<3> wz[CT];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                float v = 0.0f;
+            for (int c = 0; c < CT; ++c) {
+                f32x8 v = __builtin_convertvector(zt[s][c].p[N - 1], f32x8);
 #pragma unroll
-                for (int m = N - 1; m >= 0; --m) v += (float)zt[s].p[m][k];
-                bf16_t part[3];
-                split<3>(v * weight[32 * s + 8 * g + k], part);
-#pragma unroll
-                for (int i = 0; i < 3; ++i) wz.p[i][k] = part[i];
+                for (int m = N - 2; m >= 0; --m) v += __builtin_convertvector(zt[s][c].p[m], f32x8);
+                wz[c] = split<3>(v * w);
             }
 #pragma unroll
             for (int t = 0; t < AP / 16; ++t) {
                 Parts<N> yt;
 #pragma unroll
-                for (int m = 0; m < N; ++m) yt.p[m] = column_operand<AP>(sy + m * C * AP, 32 * s, 32 * (t / 2) + 4 * (t & 1), 8, lane);
-                M[t] = product<3>(yt, wz, M[t]);
+                for (int m = 0; m < N; ++m) yt.p[m] = column_operand<AP>(sy + m * C * AP, y_at, 32 * s, 32 * (t / 2) + 4 * (t & 1));
+#pragma unroll
+                for (int c = 0; c < CT; ++c) M[t][c] = product<3>(yt, wz[c], M[t][c]);
             }
         }
         __syncthreads();
     }
     float *to = !reads ? W.between + between : piece.last && W.m_out && slot >= 0 ? W.m_out + state : nullptr;
-    if (to && column)
-#pragma unroll
-        for (int t = 0; t < AP / 16; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const unsigned a = 32 * (t / 2) + 8 * g + 4 * (t & 1) + r;
-                if (a < W.A) to[!reads ? (size_t)a * W.E + e : (size_t)a * W.m_a + (size_t)e * W.m_e] = M[t][r];
-            }
+    const size_t m_a = reads ? W.m_a : W.E, m_e = reads ? W.m_e : 1;
+    each_of_state<AP, CT>(M, to != nullptr, e0 + wave_e, W.A, W.E, m_a, m_e, [&](float &m, size_t i) { to[i] = m; });
 }
 
 // What each segment of a row starts from, from what the segments in front of it add: a thread takes one element of the state along the row.
@@ -648,12 +702,15 @@ bool misaligned(const void *p, size_t to) { return (uintptr_t)p % to != 0; }
 
 Heads heads_of(const void *data, long long token, long long head, long long heads) { return {(void *)data, token, head, (unsigned)heads}; }
 
-template <int DT, int WAVES> const void *walk_for(unsigned A)
+template <int DT, int CT, bool WHOLE> const void *walk_for(unsigned A)
 {
-    return A <= 32 ? (const void *)walk_kernel<DT, 32, WAVES> : A <= 64 ? (const void *)walk_kernel<DT, 64, WAVES>
-         : A <= 128 ? (const void *)walk_kernel<DT, 128, WAVES> : (const void *)walk_kernel<DT, 256, WAVES>;
+    return A <= 32 ? (const void *)walk_kernel<DT, 32, CT, WHOLE> : A <= 64 ? (const void *)walk_kernel<DT, 64, CT, WHOLE>
+         : A <= 128 ? (const void *)walk_kernel<DT, 128, CT, WHOLE> : (const void *)walk_kernel<DT, 256, CT, WHOLE>;
 }
-template <int WAVES> const void *walk_for(int dt, unsigned A) { return dt == kF16 ? walk_for<kF16, WAVES>(A) : dt == kF32 ? walk_for<kF32, WAVES>(A) : walk_for<kBF16, WAVES>(A); }
+template <int CT, bool WHOLE> const void *walk_for(int dt, unsigned A)
+{
+    return dt == kF16 ? walk_for<kF16, CT, WHOLE>(A) : dt == kF32 ? walk_for<kF32, CT, WHOLE>(A) : walk_for<kBF16, CT, WHOLE>(A);
+}
 
 // Whether groups of `n` elements of every token's features are aligned and whole.
 bool whole(const Heads &x, unsigned dims, size_t esz, unsigned n)
@@ -666,22 +723,23 @@ bool whole(const Heads &x, unsigned dims, size_t esz, unsigned n)
 tcuscan_status_t walk(WalkArgs W, Heads out, float *part, int dt, hipStream_t s)
 {
     const size_t esz = elem_bytes(dt);
-    const unsigned waves = W.E <= 64 ? 4 : 8;
-    const size_t groups = (size_t)W.pieces * W.heads * ((W.E + 16 * waves - 1) / (16 * waves));
+    const unsigned tiles = W.E <= 64 ? 1 : 2, cols = 64 * tiles;
+    const size_t groups = (size_t)W.pieces * W.heads * ((W.E + cols - 1) / cols);
     const size_t join_groups = (size_t)W.rows * W.heads * (((size_t)W.A * W.E + kJoinThreads - 1) / kJoinThreads);
     if (groups > kMostBlocks || join_groups > kMostBlocks) return TCUSCAN_ERR_UNSUPPORTED;
     const bool shared = out.heads < W.heads;
     const Heads to = shared ? Heads{part, (long long)W.heads * W.E, W.E, W.heads} : out;
     W.wide = shared;
-    W.whole = whole(W.x, W.A, esz, 8) | whole(W.y, W.A, esz, 8) << 1 | whole(W.z, W.E, esz, 8) << 2 | whole(to, W.E, shared ? 4 : esz, 4) << 3;
-    const void *fn = waves == 4 ? walk_for<4>(dt, W.A) : walk_for<8>(dt, W.A);
+    const bool all_whole = whole(W.x, W.A, esz, 8) && whole(W.y, W.A, esz, 8) && whole(W.z, W.E, esz, 8) && whole(to, W.E, shared ? 4 : esz, 4);
+    const void *fn = tiles == 1 ? all_whole ? walk_for<1, true>(dt, W.A) : walk_for<1, false>(dt, W.A)
+                                : all_whole ? walk_for<2, true>(dt, W.A) : walk_for<2, false>(dt, W.A);
     if (W.segment_log2 != kWholeRows) {
         W.out = Heads{};
-        if (!launch(fn, groups, 64 * waves, &W, s) || !launch((const void *)join_kernel, join_groups, kJoinThreads, &W, s)) return TCUSCAN_ERR_HIP;
+        if (!launch(fn, groups, 64 * kWalkWaves, &W, s) || !launch((const void *)join_kernel, join_groups, kJoinThreads, &W, s)) return TCUSCAN_ERR_HIP;
     }
     W.out = to;
     if (!W.out.data) W.out.data = W.ws;            // (no tokens: nothing is written there)
-    if (!launch(fn, groups, 64 * waves, &W, s)) return TCUSCAN_ERR_HIP;
+    if (!launch(fn, groups, 64 * kWalkWaves, &W, s)) return TCUSCAN_ERR_HIP;
     const size_t items = (size_t)W.total * out.heads * W.E;
     if (!shared || !items) return TCUSCAN_OK;
     SumArgs S = {part, out, W.total, W.heads, W.E};
