@@ -97,7 +97,8 @@ __device__ __forceinline__ long long state_of(const long long *slots, unsigned r
 //
 // Precision.  The matrix unit multiplies bf16 and adds in fp32, so every operand is a sum of bf16 parts: bf16 inputs one, f16 two (exact),
 // fp32 three.  What is rounded on the way:
-//   * the weighted keys of a state: by_new a^(C-1-j) z_j in three parts (24 bits): states come out as exact as fp32 sums make them
+//   * what is added to a state, by_new a^(C-1-j) z_j: three parts (24 bits), so that states come out as exact as fp32 sums make them; two (16 bits)
+//     where only 16-bit outputs are read from it
 //   * the state, where it is read: two parts (16 bits), three for fp32
 //   * the weighted scores P: one part for bf16 (an error like the output's own rounding), two for f16, three for fp32
 // and products of parts that together lie below what is kept are left out (kOrder).
@@ -131,15 +132,15 @@ template <int N> __device__ __forceinline__ Parts<N> split(f32x8 x)
     }
     return parts;
 }
-// acc += a b for sums of parts: all products a[i] b[j] with i + j < kOrder.
-template <int kOrder, int NA, int NB> __device__ __forceinline__ f32x4 product(const Parts<NA> &a, const Parts<NB> &b, f32x4 acc)
+__device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 acc) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, acc, 0, 0, 0); }
+// A product of sums of parts: step(i, j) for all products a[i] b[j] with i + j < kOrder, small ones first.
+template <int kOrder, class Step, int NA, int NB> __device__ __forceinline__ void products(Step step, const Parts<NA> &, const Parts<NB> &)
 {
 #pragma unroll
     for (int i = NA - 1; i >= 0; --i)
 #pragma unroll
         for (int j = NB - 1; j >= 0; --j)
-            if (i + j < kOrder) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[j], acc, 0, 0, 0);
-    return acc;
+            if (i + j < kOrder) step(i, j);
 }
 
 // Tiles in LDS are rows of COLS bf16 whose 16-byte granules are permuted within each row by an exclusive or with a number made of the row.  The
@@ -373,6 +374,9 @@ template <int DT, int AP, int CT, bool WHOLE> __global__ __launch_bounds__(64 * 
     const int out_size = W.wide ? 4 : (int)sizeof(T);
     char *out = (char *)W.out.data + (W.out.at(h, W.heads) + (origin + sign * l) * W.out.token + e0 + wave_e + 4 * g) * out_size;
     const long long out_step = sign * 16 * W.out.token * out_size;
+    float *to = !reads ? W.between + between : piece.last && W.m_out && slot >= 0 ? W.m_out + state : nullptr;
+    // the third part of what is added to a state counts where the state itself is asked for, not where 16-bit outputs are read from it
+    const bool exact = to || DT == kF32;
     const long long length = piece.end - piece.first;
     auto fetch = [&](long long left) {
         const int n = (int)(left < C ? left : C);
@@ -406,11 +410,11 @@ template <int DT, int AP, int CT, bool WHOLE> __global__ __launch_bounds__(64 * 
                         a.p[m] = row_operand<AP>(sy + m * C * AP, row_at, 16 * jt, 32 * s);
                         b.p[m] = row_operand<AP>(sx + m * C * AP, row_at, 16 * it, 32 * s);
                     }
-                    p = product<kOrder>(a, b, p);
+                    products<kOrder>([&](int i, int j) { p = mfma(a.p[i], b.p[j], p); }, a, b);
                 }
-                const int i = 16 * it + l, j = 16 * jt + 4 * g;
+                const int i = 16 * it + l, j = 16 * jt + 4 * g, apart = here(i - j);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) p[r] = j + r <= i ? p[r] * (W.by_new * decay_power(log_decay, (float)(i - j - r))) : 0.0f;
+                for (int r = 0; r < 4; ++r) p[r] = apart >= r ? p[r] * (W.by_new * decay_power(log_decay, (float)(apart - r))) : 0.0f;
 #pragma unroll
                 for (int m = 0; m < N; ++m) {
                     const bf16x4 part = __builtin_convertvector(p, bf16x4);
@@ -437,30 +441,39 @@ template <int DT, int AP, int CT, bool WHOLE> __global__ __launch_bounds__(64 * 
 #pragma unroll
             for (int s = 0; s < AP / 32; ++s) {
                 __builtin_amdgcn_sched_barrier(0);             // (or the parts of all steps take registers at once)
+                Parts<N> b[kTiles];
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                    for (int i = 0; i < N; ++i) b[t].p[i] = row_operand<AP>(sx + i * C * AP, row_at, 16 * t, 32 * s);
                 Parts<NM> m[CT];
 #pragma unroll
                 for (int c = 0; c < CT; ++c) m[c] = split<NM>(__builtin_shufflevector(M[2 * s][c], M[2 * s + 1][c], 0, 1, 2, 3, 4, 5, 6, 7));
+                products<kOrder>([&](int i, int j) {           // (independent ones behind each other)
 #pragma unroll
-                for (int t = 0; t < kTiles; ++t) {
-                    Parts<N> b;
+                    for (int c = 0; c < CT; ++c)
 #pragma unroll
-                    for (int i = 0; i < N; ++i) b.p[i] = row_operand<AP>(sx + i * C * AP, row_at, 16 * t, 32 * s);
-#pragma unroll
-                    for (int c = 0; c < CT; ++c) o[t][c] = product<kOrder>(m[c], b, o[t][c]);
-                }
+                        for (int t = 0; t < kTiles; ++t) o[t][c] = mfma(m[c].p[i], b[t].p[j], o[t][c]);
+                }, m[0], b[0]);
             }
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t) {
+            for (int t = 0; t < kTiles; ++t)
 #pragma unroll
                 for (int c = 0; c < CT; ++c) o[t][c] *= reading[t];
 #pragma unroll
-                for (int s = 0; s <= t / 2; ++s) {
-                    Parts<N> b;
+            for (int s = 0; s < kSteps; ++s) {
+                Parts<N> b[kTiles];
 #pragma unroll
-                    for (int i = 0; i < N; ++i) b.p[i] = row_operand<C>(sp + i * C * C, p_at, 16 * t, 32 * s);
+                for (int t = 2 * s; t < kTiles; ++t)
 #pragma unroll
-                    for (int c = 0; c < CT; ++c) o[t][c] = product<kOrder>(zt[s][c], b, o[t][c]);
-                }
+                    for (int i = 0; i < N; ++i) b[t].p[i] = row_operand<C>(sp + i * C * C, p_at, 16 * t, 32 * s);
+                products<kOrder>([&](int i, int j) {
+#pragma unroll
+                    for (int t = 2 * s; t < kTiles; ++t)
+#pragma unroll
+                        for (int c = 0; c < CT; ++c) o[t][c] = mfma(zt[s][c].p[i], b[t].p[j], o[t][c]);
+                }, zt[0][0], b[0]);
             }
 #pragma unroll
             for (int t = 0; t < kTiles; ++t, out += out_step) {
@@ -501,17 +514,26 @@ template <int DT, int AP, int CT, bool WHOLE> __global__ __launch_bounds__(64 * 
                 wz[c] = split<3>(v * w);
             }
 #pragma unroll
-            for (int t = 0; t < AP / 16; ++t) {
-                Parts<N> yt;
+            for (int t = 0; t < AP / 16; t += 2) {
+                Parts<N> yt[2];
 #pragma unroll
-                for (int m = 0; m < N; ++m) yt.p[m] = column_operand<AP>(sy + m * C * AP, y_at, 32 * s, 32 * (t / 2) + 4 * (t & 1));
+                for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int c = 0; c < CT; ++c) M[t][c] = product<3>(yt, wz[c], M[t][c]);
+                    for (int m = 0; m < N; ++m) yt[u].p[m] = column_operand<AP>(sy + m * C * AP, y_at, 32 * s, 16 * t + 4 * u);
+                auto add = [&](int i, int j) {
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int c = 0; c < CT; ++c) M[t + u][c] = mfma(yt[u].p[i], wz[c].p[j], M[t + u][c]);
+                };
+                if (exact)
+#pragma unroll
+                    for (int i = 0; i < N; ++i) add(i, 2 - i);
+                products<2>(add, yt[0], Parts<2>());
             }
         }
         __syncthreads();
     }
-    float *to = !reads ? W.between + between : piece.last && W.m_out && slot >= 0 ? W.m_out + state : nullptr;
     const size_t m_a = reads ? W.m_a : W.E, m_e = reads ? W.m_e : 1;
     each_of_state<AP, CT>(M, to != nullptr, e0 + wave_e, W.A, W.E, m_a, m_e, [&](float &m, size_t i) { to[i] = m; });
 }
