@@ -1,0 +1,962 @@
+// Linear attention with one decay per head: the prefix sum with a matrix for an element and a decay between elements.
+//
+// For one row of tokens and one head, with a = exp(log_decay):
+//
+//   forward  : S_t = a S_(t-1) + k_t v_t^T,   o_t = scale q_t S_t            (S: dk x dv, S_(-1) = state_in, q_t a row vector)
+//   gradients: with R_t = scale q_t^T do_t + a R_(t+1)  (R_(T) = d_state_out / a, so that R_(T-1) = scale q^T do + d_state_out)
+//              dq_t = scale do_t S_t^T,  dv_t = k_t R_t,  dk_t = v_t R_t^T,  d_state_in = a R_0
+//
+// All four are one operator, "walk": a state M (A x E) that takes y_t z_t^T token by token and is read as x_t M, from the front
+//   M_t = a M_(t-1) + by_new y_t z_t^T;  out_t = by_read x_t M_t
+// or from the end, where the state decays after the token rather than before it
+//   M_t = M_(t+1) + by_new y_t z_t^T;  out_t = by_read x_t M_t;  M_t *= a
+//   o: (q, k, v) from the front, M = S;    dq: (do, v, k) from the front, M = S^T
+//   dv: (k, q, do) from the end, M = R;    dk: (v, do, q) from the end, M = R^T
+// Stored heads that several heads share give each of them a walk; gradients of shared heads are summed over them afterwards.
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "../../include/tcuscan.h"
+#include "chain_layout.h"
+#include "element_types.h"
+
+namespace {
+
+constexpr int kMaxDim = 256;
+
+// One of the arrays [token][stored head][feature]: head h is the stored head h * heads / all heads.
+struct Heads {
+    void *data;
+    long long token, head;                         // strides in elements
+    unsigned heads;
+    __device__ __forceinline__ long long at(unsigned h, unsigned all) const { return (long long)(h * (unsigned long long)heads / all) * head; }
+};
+
+__device__ unsigned long long g_prof[16];
+struct WalkArgs {
+    Heads x, y, z, out;                            // out.heads is the number of heads
+    const float *log_decay;
+    const long long *offsets, *slots;              // slots: null, or the state that each row has
+    const float *m_in;                             // null: zeros
+    float *m_out;                                  // null: not wanted
+    float *between;                                // [piece][head][A][E]: what segments add, then what they start from
+    void *ws;
+    long long states;                              // how many states there are
+    long long total;
+    unsigned rows, heads, A, E;
+    unsigned m_a, m_e;                             // strides of a state: M[a][e] is at a * m_a + e * m_e
+    unsigned pieces, segment_log2;
+    float by_new, by_read;
+    int from_end;
+    int wide;                                      // the output is fp32 whatever the element type
+};
+
+// a^n, for weights.  (An n of 0 gives 1 for a decay of 0, a log_decay of minus infinity, too.)
+__device__ __forceinline__ float decay_power(float log_decay, float n) { return __expf(fmaxf(log_decay, -1e30f) * n); }
+// Takes a state n tokens on: m becomes a^n m.  Slow decays (a^n from 1/2 on) as m + (a^n - 1) m: multiplied by a rounded a^n, a state
+// would be off by up to half a unit in the last place of 1 each time, always to the same side: 1e-5 for 1 - 2^-9 token by token.
+struct Decay {
+    float by;
+    bool slow;
+    __device__ __forceinline__ Decay(float log_decay, float n)
+    {
+        const float x = fmaxf(log_decay, -1e30f) * n;
+        slow = x > -0.69f;
+        by = slow ? expm1f(x) : __expf(x);
+    }
+    __device__ __forceinline__ float operator()(float m) const { return fmaf(m, by, slow ? m : 0.0f); }
+};
+
+// Row r's tokens, clipped to the arrays.
+__device__ __forceinline__ void row_extent(const long long *offsets, unsigned r, long long total, long long &lo, long long &hi)
+{
+    lo = offsets[r]; hi = offsets[r + 1];
+    lo = lo < 0 ? 0 : lo > total ? total : lo;
+    hi = hi < lo ? lo : hi > total ? total : hi;
+}
+
+// Row r's place among the states, or -1 for none.
+__device__ __forceinline__ long long state_of(const long long *slots, unsigned r, long long states)
+{
+    const long long s = slots ? slots[r] : (long long)r;
+    return s >= 0 && s < states ? s : -1;
+}
+
+// ---------------------------------------------------------------- the walk in blocks of tokens, on the matrix unit
+//
+// C tokens i = 0 .. C-1 of a row (from the end: the last token first) with the state M in front of them:
+//
+//   out_i = by_read (a^(i+1) x_i M + sum over j <= i of by_new a^(i-j) (x_i . y_j) z_j)    (from the end a^i in place of a^(i+1))
+//   M    <- a^C M + sum over j of by_new a^(C-1-j) y_j^T z_j                          (from the end a^(C-j))
+//
+// Every sum over features or tokens is a matrix product: P^T = Y X^T (then weighted and cut to j <= i), out^T = M^T X^T and Z^T P^T,
+// M += Y^T (wZ).  A wavefront owns 16 CT columns of Z, out and M and all A rows of M, in MFMA accumulators from the first token to the
+// last.  The products are ordered so that operands fall into the lanes that have them: the accumulators of M, two row tiles side by side, are
+// the left operand of M^T X^T as they stand (tile rows are dealt so that a lane's eight values are eight consecutive a), and Z's columns are
+// read transposed once, for Z^T P^T and, weighted, for the update.  Only X, Y, Z (shared by all wavefronts of the workgroup) and P go through LDS.
+//
+// Precision.  The matrix unit multiplies bf16 and adds in fp32, so every operand is a sum of bf16 parts: bf16 inputs one, f16 two (exact),
+// fp32 three.  What is rounded on the way:
+//   * what is added to a state, by_new a^(C-1-j) z_j: three parts (24 bits), so that states come out as exact as fp32 sums make them; two (16 bits)
+//     where only 16-bit outputs are read from it
+//   * the state, where it is read: two parts (16 bits), three for fp32
+//   * the weighted scores P: one part for bf16 (an error like the output's own rounding), two for f16, three for fp32
+// and products of parts that together lie below what is kept are left out (kOrder).
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short  s16x4 __attribute__((ext_vector_type(4)));
+typedef short  s16x8 __attribute__((ext_vector_type(8)));
+typedef float  f32x4 __attribute__((ext_vector_type(4)));
+typedef float  f32x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int parts_of(int dt) { return dt == kBF16 ? 1 : dt == kF16 ? 2 : 3; }
+// Tokens of a block: what LDS holds of X, Y and Z next to each other.
+constexpr int block_tokens(int dt, int ap) { return dt == kF32 || (dt == kF16 && ap > 128) ? 32 : 64; }
+
+constexpr int kWalkWaves = 4;
+constexpr int kLoadsDone = 0x0F70;                 // s_waitcnt: no load or store on its way, whatever else is
+// Workgroups on a compute unit, by what LDS and registers give.
+constexpr int groups_at_once(int dt, int ap, int ct) { return ap > 128 || (dt != kBF16 && ap > 64) || (dt == kF16 && ct > 1) ? 1 : 2; }
+
+template <int N> struct Parts { bf16x8 p[N]; };
+
+// The first N bf16 parts of eight values: x = part 0 + part 1 + ..., each the rounding of what the ones before leave.
+template <int N> __device__ __forceinline__ Parts<N> split(f32x8 x)
+{
+    Parts<N> parts;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        parts.p[n] = __builtin_convertvector(x, bf16x8);
+        x -= __builtin_convertvector(parts.p[n], f32x8);
+    }
+    return parts;
+}
+__device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 acc) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, acc, 0, 0, 0); }
+// A product of sums of parts: step(i, j) for all products a[i] b[j] with i + j < kOrder, small ones first.
+template <int kOrder, class Step, int NA, int NB> __device__ __forceinline__ void products(Step step, const Parts<NA> &, const Parts<NB> &)
+{
+#pragma unroll
+    for (int i = NA - 1; i >= 0; --i)
+#pragma unroll
+        for (int j = NB - 1; j >= 0; --j)
+            if (i + j < kOrder) step(i, j);
+}
+
+// Tiles in LDS are rows of COLS bf16 whose 16-byte granules are permuted within each row by an exclusive or with a number made of the row.  The
+// permutation keeps both kinds of reading free of bank conflicts: the same granule of 16 consecutive rows (row operands), and four
+// granules of four consecutive rows (operands read transposed).
+template <int COLS> struct Tile {
+    static constexpr int kGranules = COLS / 8;
+    __device__ __forceinline__ static int swizzle(int row)
+    {
+        if constexpr (kGranules >= 16) return (row & 3) << 2 | ((row >> 2) & 3);
+        else if constexpr (kGranules == 8) return ((row >> 1) & 1) << 2 | ((row >> 2) & 3);
+        else return (row >> 2) & 3;
+    }
+    __device__ __forceinline__ static int at(int row, int col) { return row * COLS + ((((col >> 3) ^ swizzle(row)) << 3) | (col & 7)); }
+};
+
+// Where a lane finds operands.  Both kinds of reading go through one number per lane and tile shape; the operand's place in the tile then is an exclusive or
+// with a constant (columns) and a constant offset (rows, which the swizzle repeats every 16 of).
+//
+// Row operand: lane l of group g receives the eight columns k0 + 8 g .. + 7 of row row0 + l (row0 a multiple of 16, k0 of 32).
+template <int COLS> __device__ __forceinline__ int row_lane(int lane) { return Tile<COLS>::at(lane & 15, 8 * (lane >> 4)); }
+template <int COLS> __device__ __forceinline__ bf16x8 row_operand(const bf16_t *tile, int mine, int row0, int k0) { return *(const bf16x8 *)(tile + row0 * COLS + (mine ^ k0)); }
+// Column operand: lane l of group g receives one column of the eight rows row0 + 8 g .. + 7 (row0 a multiple of 32).  The instruction hands lane l of 16 the
+// l-th column of the four rows whose 16 pieces of four columns the 16 lanes point at: lane s at row s / 4 and piece s % 4, which starts PIECE columns behind the
+// one before.  `first`: the wavefront's first column, a multiple of 32 (of 16, if it is the only one); col0: from there, a multiple of 16 or with PIECE = 8
+// of 32, and there + 4 for the other halves of the pieces' granules.
+__device__ __forceinline__ s16x4 read_transposed(const bf16_t *p)
+{
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)p);
+}
+template <int COLS, int PIECE> __device__ __forceinline__ int column_lane(int lane, int first) { return Tile<COLS>::at(8 * (lane >> 4) + ((lane & 15) >> 2), first + PIECE * (lane & 3)); }
+template <int COLS> __device__ __forceinline__ bf16x8 column_operand(const bf16_t *tile, int mine, int row0, int col0)
+{
+    const bf16_t *p = tile + row0 * COLS + (col0 & 4);
+    const int at = mine ^ (col0 & ~4);             // four rows on, the swizzle differs in its lowest bit
+    const s16x4 a = read_transposed(p + at), b = read_transposed(p + 4 * COLS + (at ^ 8));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+// Keeps the compiler from computing what depends on v ahead of a loop: addresses made of a lane's number and constants would take dozens of registers.
+__device__ __forceinline__ int here(int v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
+// A block of tokens on its way from memory to LDS: C rows of COLS elements, a granule of eight to a lane at a time.  Rows from n on and columns from `cols`
+// on become zeros.  Three ways:
+//   kDirect   bf16, granules aligned and either inside or outside: loads that write LDS themselves, lane after lane, so that it is the lanes' addresses
+//             that are permuted; what is outside is beyond the end of the buffer they read from.  They need no registers while they are on
+//             their way (held there, the 48 a lane would need at dk = dv = 128 are spilled).
+//   kStaged   fp32 and f16, granules as above: through registers, split into parts on the way.
+//   kSlow     anything else: element by element.
+enum Way { kDirect, kStaged, kSlow };
+constexpr Way way_of(int dt, bool whole) { return !whole ? kSlow : dt == kBF16 ? kDirect : kStaged; }
+template <int DT, int C, int COLS, int THREADS, bool WHOLE> struct Stage {
+    typedef typename Elem<DT>::T T;
+    static constexpr Way kWay = way_of(DT, WHOLE);
+    static constexpr int kItems = C * COLS / 8, kEach = (kItems + THREADS - 1) / THREADS, kQuads = sizeof(T) / 2, N = parts_of(DT);
+    static constexpr int kRowsAtOnce = THREADS / (COLS / 8);
+    static_assert(THREADS % (COLS / 8) == 0, "a lane keeps to its columns");
+    static constexpr int kOffsets = kRowsAtOnce % 16 == 0 ? 1 : 2;             // the swizzle repeats every 16 rows
+    static_assert(kRowsAtOnce % 8 == 0, "or every second time");
+    u32x4 v[kWay == kStaged ? kEach : 1][kQuads];
+    const T *first;                                // the block's first row (the same for all lanes)
+    long long step;                                // from row to row
+    int row, col, cols;
+    int offset[kOffsets];                          // kDirect: the lane's first granules in a whole block, in bytes from its lowest address
+
+    __device__ __forceinline__ void begin(const T *p, long long row_step, int columns)
+    {
+        row = (int)threadIdx.x / (COLS / 8); col = (int)threadIdx.x % (COLS / 8) * 8; cols = columns; first = p; step = row_step;
+        if constexpr (kWay == kDirect)
+#pragma unroll
+            for (int i = 0; i < kOffsets; ++i) {
+                const int r = row + i * kRowsAtOnce, c = (int)(threadIdx.x % (COLS / 8) ^ Tile<COLS>::swizzle(r)) * 8;
+                offset[i] = c < cols ? ((step < 0 ? C - 1 - r : r) * (int)(step < 0 ? -step : step) + c) * (int)sizeof(T) : kOutside;
+            }
+    }
+    static constexpr int kOutside = 1 << 30;       // beyond the end of any block (64 rows less than 2^22 elements apart)
+    // kDirect: all the way, to be waited for; kStaged: as far as the registers.
+    __device__ __forceinline__ void load(bf16_t *tile, int n)
+    {
+        if constexpr (kWay == kDirect) {
+            const int by_row = (int)(step < 0 ? -step : step) * (int)sizeof(T), shift = step < 0 ? (C - n) * by_row : 0;
+            const __amdgpu_buffer_rsrc_t block = __builtin_amdgcn_make_buffer_rsrc((void *)(step < 0 ? first + (n - 1) * step : first), 0, (n - 1) * by_row + cols * (int)sizeof(T), 0x00027000);
+            bf16_t *to = tile + __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64) * 512;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const int at = offset[i % kOffsets] + (i - i % kOffsets) * kRowsAtOnce * (step < 0 ? -by_row : by_row) - shift;
+                if (kEach * THREADS <= kItems || (int)threadIdx.x < kItems)
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(block, (__attribute__((address_space(3))) void *)(to + i * THREADS * 8), 16, at, 0, 0, 0);
+            }
+            first += C * step;
+        } else if constexpr (kWay == kStaged) {
+            const T *p = first + row * step + col;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i, p += kRowsAtOnce * step) {
+#pragma unroll
+                for (int q = 0; q < kQuads; ++q) v[i][q] = u32x4{0u, 0u, 0u, 0u};
+                if (row + i * kRowsAtOnce < n && col < cols)
+#pragma unroll
+                    for (int q = 0; q < kQuads; ++q) v[i][q] = ((const u32x4 *)p)[q];
+            }
+        }
+    }
+    static __device__ __forceinline__ void put(bf16_t *to, const T (&e)[8])                       // the parts are C * COLS elements apart
+    {
+        if constexpr (N == 1) {
+            __builtin_memcpy(to, e, 16);
+        } else {
+            f32x8 x;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = (float)e[k];
+            const Parts<N> parts = split<N>(x);
+#pragma unroll
+            for (int n = 0; n < N; ++n) *(bf16x8 *)(to + n * C * COLS) = parts.p[n];
+        }
+    }
+    // kStaged and kSlow: the rest of the way, and on to the next block.
+    __device__ __forceinline__ void store(bf16_t *tile, int n)
+    {
+        if constexpr (kWay == kStaged) {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                T e[8];
+                __builtin_memcpy(e, &v[i][0], sizeof e);
+                if (row + i * kRowsAtOnce < C) put(tile + Tile<COLS>::at(row + i * kRowsAtOnce, col), e);
+            }
+        } else if constexpr (kWay == kSlow) {
+#pragma unroll 1
+            for (int r = row; r < C; r += kRowsAtOnce) {
+                const T *p = first + r * step + col;
+                T e[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) e[k] = r < n && col + k < cols ? p[k] : (T)0.0f;
+                put(tile + Tile<COLS>::at(r, col), e);
+            }
+        }
+        first += C * step;
+    }
+};
+
+// Which piece of which row a workgroup walks over.  Rows are cut into segments of 2^segment_log2 tokens; the segments of row r have the numbers
+// from offsets[r] / 2^segment_log2 + r on, which leaves every row room for its own without anything being counted first.
+struct Piece {
+    unsigned r;
+    long long lo, hi;                              // the row's tokens
+    long long first, end;                          // the segment's, counted from where the walk starts
+    bool last;
+};
+__device__ __forceinline__ long long uniform(long long v)
+{   // (the same in all lanes: into scalar registers)
+    return (long long)((unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)v));
+}
+__device__ __forceinline__ bool find_piece(const WalkArgs &W, unsigned number, Piece &p)
+{
+    unsigned lo = 0, hi = W.rows;
+    const bool one = (W.total >> W.segment_log2) == 0;       // a row is one segment
+    if (one) {
+        lo = number;
+    } else {
+        while (hi - lo > 1) {                      // the last row whose segments start at or below `number`
+            const unsigned mid = lo + (hi - lo) / 2;
+            if ((W.offsets[mid] >> W.segment_log2) + mid <= (long long)number) lo = mid; else hi = mid;
+        }
+    }
+    p.r = lo;
+    row_extent(W.offsets, p.r, W.total, p.lo, p.hi);
+    p.lo = uniform(p.lo); p.hi = uniform(p.hi);
+    const long long length = p.hi - p.lo, s = one ? 0 : (long long)number - (p.lo >> W.segment_log2) - p.r, segment = 1ll << W.segment_log2;
+    p.first = s * segment;
+    if (s < 0 || (s > 0 && p.first >= length)) return false;
+    p.end = p.first + segment < length ? p.first + segment : length;
+    p.last = p.end == length;
+    return true;
+}
+
+// K consecutive columns of the output, `col` the first of them.  WHOLE: they are aligned and all inside or all outside.
+template <class T, bool WHOLE, int K> __device__ __forceinline__ void store_columns(T *p, int col, int cols, const f32x4 *v, float by)
+{
+    typedef T Some __attribute__((ext_vector_type(K)));
+    Some x;
+#pragma unroll
+    for (int k = 0; k < K; ++k) x[k] = (T)(v[k / 4][k % 4] * by);
+    if constexpr (WHOLE) {
+        if (col < cols) *(Some *)p = x;
+    } else {
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (col + k < cols) p[k] = x[k];
+    }
+}
+
+// Calls what(element, its index) for the lane's elements of a state that exist.  The lane's number passes through an empty asm statement: otherwise
+// the compiler keeps every element's address and predicate from the reading of a state to its writing, registers that the walk needs.
+template <int AP, int CT, class What> __device__ __forceinline__ void each_of_state(f32x4 (&M)[AP / 16][CT], bool any, unsigned first_e, unsigned A, unsigned E, size_t m_a,
+                                                                                    size_t m_e, What what)
+{
+    unsigned lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    if (!any) return;
+    const unsigned a0 = 8 * (lane >> 4), e_lane = first_e + 4 * CT * ((lane & 15) >> 2) + (lane & 3);
+#pragma unroll
+    for (int t = 0; t < AP / 16; ++t)
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const unsigned a = a0 + 32 * (t / 2) + 4 * (t & 1) + r, e = e_lane + 4 * c;
+                float m = M[t][c][r];
+                if (a < A && e < E) what(m, a * m_a + e * m_e);
+                M[t][c][r] = m;
+            }
+}
+
+template <int DT, int AP, int CT, bool WHOLE> __global__ __launch_bounds__(64 * kWalkWaves, groups_at_once(DT, AP, CT)) void walk_kernel(WalkArgs W)
+{
+    typedef typename Elem<DT>::T T;
+    constexpr int N = parts_of(DT), C = block_tokens(DT, AP), EB = 16 * kWalkWaves * CT, kThreads = 64 * kWalkWaves;
+    constexpr bool kDirectly = way_of(DT, WHOLE) == kDirect;
+    constexpr int kTiles = C / 16, kSteps = C / 32, kOrder = N == 3 ? 3 : 2;       // tiles of 16 tokens, steps of 32
+    __shared__ __attribute__((aligned(16))) bf16_t sx[N * C * AP], sy[(kDirectly ? 2 : 1) * N * C * AP], sz[N * C * EB], sp[N * C * C];
+    __shared__ __attribute__((aligned(16))) float weight[C];
+
+    const unsigned blocks = (W.E + EB - 1) / EB;
+    const unsigned block = blockIdx.x % blocks, h = blockIdx.x / blocks % W.heads, number = blockIdx.x / blocks / W.heads;
+    const int lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    if (block == 0 && h == 0)                      // offsets and slots are looked over once
+        for (size_t r = (size_t)number * kThreads + threadIdx.x; r < W.rows; r += (size_t)W.pieces * kThreads) {
+            const long long a = W.offsets[r], b = W.offsets[r + 1];
+            if (a < 0 || b < a || b > W.total || (W.slots && W.slots[r] >= W.states)) raise_fault(W.ws, kFaultBadIndex);
+        }
+    Piece piece;
+    if (!find_piece(W, number, piece)) return;
+    const bool reads = W.out.data != nullptr;
+    if (!reads && piece.last) return;              // (what a row's last segment adds, nobody asks for)
+
+    const float log_decay = W.log_decay[h];
+    const int e0 = (int)block * EB, wave_e = 16 * CT * wave;        // the workgroup's first column, and the wavefront's of these
+    const long long slot = state_of(W.slots, piece.r, W.states);
+    const size_t state = ((size_t)slot * W.heads + h) * W.A * W.E, between = ((size_t)number * W.heads + h) * W.A * W.E;
+    const bool cut = piece.first > 0 || !piece.last;                // a row of several segments
+    // M[2 s + t][c][r] is M[a][e] with a = 32 s + 8 g + 4 t + r, e = e0 + wave_e + 4 CT (l / 4) + 4 c + l % 4: the columns of a lane's outputs are
+    // then next to each other
+    f32x4 M[AP / 16][CT] = {};
+    {
+        // a row of several segments finds what it starts from in the workspace, also for the first of them
+        const float *from = !reads ? nullptr : cut ? W.between + between : W.m_in && slot >= 0 ? W.m_in + state : nullptr;
+        const size_t m_a = cut ? W.E : W.m_a, m_e = cut ? 1 : W.m_e;
+        each_of_state<AP, CT>(M, from != nullptr, e0 + wave_e, W.A, W.E, m_a, m_e, [&](float &m, size_t i) { m = from[i]; });
+    }
+    float reading[kTiles];                         // a^(i+1), from the end a^i, of the lane's token in each tile
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) reading[t] = decay_power(log_decay, (float)(16 * t + l + (W.from_end ? 0 : 1)));
+    if (reads)                                     // P above its diagonal of tiles: zeros for good
+        for (int i = threadIdx.x; i < N * (C / 32) * 16 * 2; i += kThreads) {
+            const int n = i / (C / 32 * 32), t = i / 32 % (C / 32), row = i / 2 % 16, half = i % 2;
+            *(u32x4 *)(sp + n * C * C + Tile<C>::at(32 * t + row, 32 * t + 16 + 8 * half)) = u32x4{0u, 0u, 0u, 0u};
+        }
+
+    const long long sign = W.from_end ? -1 : 1, origin = (W.from_end ? piece.hi - 1 : piece.lo) + sign * piece.first;
+    Stage<DT, C, AP, kThreads, WHOLE> next_x, next_y;
+    Stage<DT, C, EB, kThreads, WHOLE> next_z;
+    next_x.begin((const T *)W.x.data + W.x.at(h, W.heads) + origin * W.x.token, sign * W.x.token, (int)W.A);
+    next_y.begin((const T *)W.y.data + W.y.at(h, W.heads) + origin * W.y.token, sign * W.y.token, (int)W.A);
+    next_z.begin((const T *)W.z.data + W.z.at(h, W.heads) + origin * W.z.token + e0, sign * W.z.token, (int)W.E - e0);
+    // the lane's first output: token l of the block, column 4 CT g of the wavefront's
+    const int out_size = W.wide ? 4 : (int)sizeof(T), col = e0 + wave_e + 4 * CT * g;
+    const long long out_step = sign * W.out.token * out_size;
+    char *out = (char *)W.out.data + (W.out.at(h, W.heads) + origin * W.out.token) * out_size + (sign < 0 ? 15 * out_step : 0);
+    typedef std::conditional_t<WHOLE, unsigned, long long> Offset;
+    const Offset out_lane = (Offset)((sign < 0 ? l - 15 : l) * out_step) + (Offset)(col * out_size);         // (not negative: outputs have positive strides)
+    float *to = !reads ? W.between + between : piece.last && W.m_out && slot >= 0 ? W.m_out + state : nullptr;
+    // the third part of what is added to a state counts where the state itself is asked for, not where 16-bit outputs are read from it
+    const bool exact = to || DT == kF32;
+    const long long length = piece.end - piece.first;
+    // the next block: Y has two tiles in LDS if loads write there themselves, X and Z have been read before these start
+    auto fetch = [&](long long left, bf16_t *y_tile) {
+        const int n = (int)(left < C ? left : C);
+        if (reads) next_x.load(sx, n);
+        next_y.load(y_tile, n);
+        next_z.load(sz, n);
+    };
+    auto write_weights = [&](int n) {
+        if ((int)threadIdx.x < C)
+            weight[threadIdx.x] = (int)threadIdx.x < n ? W.by_new * decay_power(log_decay, (float)(n - 1 - (int)threadIdx.x + (W.from_end ? 1 : 0))) : 0.0f;
+    };
+    if (length > 0) fetch(length, sy);
+    write_weights((int)(length < C ? length : C));
+    int half = 0;                                  // the tile of Y in use
+    for (long long at = 0; at < length; at += C, half ^= kDirectly) {
+        const int n = (int)(length - at < C ? length - at : C);
+        bf16_t *const y_now = sy + half * C * AP;
+        const int row_at = here(row_lane<AP>(lane)), p_at = here(row_lane<C>(lane)), y_at = here(column_lane<AP, 8>(lane, 0)), z_at = here(column_lane<EB, 4 * CT>(lane, wave_e));
+        if constexpr (kDirectly) {
+            __builtin_amdgcn_s_waitcnt(kLoadsDone);
+        } else {
+            __syncthreads();                       // everybody has done with the block before
+            if (reads) next_x.store(sx, n);
+            next_y.store(sy, n);
+            next_z.store(sz, n);
+        }
+        __syncthreads();
+        if (n < C && at > 0) write_weights(n);     // (everybody has done with the block before, and reads them behind the next barrier)
+        if (reads) {
+            // P^T, 16 keys by 16 queries at a time: the wavefronts take every fourth of the tiles on and below the diagonal, each all of its own at once
+            constexpr int kPTiles = kTiles * (kTiles + 1) / 2, kMine = (kPTiles + kWalkWaves - 1) / kWalkWaves;
+            int it[kMine], jt[kMine];
+            f32x4 p[kMine];
+#pragma unroll
+            for (int k = 0; k < kMine; ++k) {
+                const int tile = min(wave + k * kWalkWaves, kPTiles - 1);
+                it[k] = tile >= 6 ? 3 : tile >= 3 ? 2 : tile >= 1 ? 1 : 0;
+                jt[k] = tile - it[k] * (it[k] + 1) / 2;
+                p[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            }
+#pragma unroll
+            for (int s = 0; s < AP / 32; ++s)
+#pragma unroll
+                for (int k = 0; k < kMine; ++k) {
+                    Parts<N> a, b;
+#pragma unroll
+                    for (int m = 0; m < N; ++m) {
+                        a.p[m] = row_operand<AP>(y_now + m * C * AP, row_at, 16 * jt[k], 32 * s);
+                        b.p[m] = row_operand<AP>(sx + m * C * AP, row_at, 16 * it[k], 32 * s);
+                    }
+                    products<kOrder>([&](int i, int j) { p[k] = mfma(a.p[i], b.p[j], p[k]); }, a, b);
+                }
+#pragma unroll
+            for (int k = 0; k < kMine; ++k) {
+                const int i = 16 * it[k] + l, j = 16 * jt[k] + 4 * g, apart = here(i - j);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) p[k][r] = apart >= r ? p[k][r] * (W.by_new * decay_power(log_decay, (float)(apart - r))) : 0.0f;
+#pragma unroll
+                for (int m = 0; m < N; ++m) {
+                    const bf16x4 part = __builtin_convertvector(p[k], bf16x4);
+                    if (wave + k * kWalkWaves < kPTiles) *(bf16x4 *)(sp + m * C * C + Tile<C>::at(i, j)) = part;
+                    p[k] -= __builtin_convertvector(part, f32x4);
+                }
+            }
+        { asm volatile("" ::: "memory"); __builtin_amdgcn_sched_barrier(0); unsigned long long now_ = __builtin_readcyclecounter(); if (reads) acc_[2] += now_ - last_; last_ = now_; __builtin_amdgcn_sched_barrier(0); }
+            __syncthreads();
+        { asm volatile("" ::: "memory"); __builtin_amdgcn_sched_barrier(0); unsigned long long now_ = __builtin_readcyclecounter(); if (reads) acc_[3] += now_ - last_; last_ = now_; __builtin_amdgcn_sched_barrier(0); }
+        }
+        Parts<N> zt[kSteps][CT];                   // 16 columns of Z by 32 tokens
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+            for (int c = 0; c < CT; ++c)
+#pragma unroll
+                for (int m = 0; m < N; ++m) zt[s][c].p[m] = column_operand<EB>(sz + m * C * EB, z_at, 32 * s, 4 * c);
+        constexpr int NM = N == 3 ? 3 : 2;
+        f32x4 o[kTiles][CT];
+        if (reads) {
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                for (int c = 0; c < CT; ++c) o[t][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            Parts<NM> m[2][CT];                    // this step's parts of M and the next one's
+            auto split_m = [&](int s) {
+#pragma unroll
+                for (int c = 0; c < CT; ++c) m[s & 1][c] = split<NM>(__builtin_shufflevector(M[2 * s][c], M[2 * s + 1][c], 0, 1, 2, 3, 4, 5, 6, 7));
+            };
+            split_m(0);
+#pragma unroll
+            for (int s = 0; s < AP / 32; ++s) {
+                __builtin_amdgcn_sched_barrier(0);             // (or the parts of all steps take registers at once)
+                Parts<N> b[kTiles];
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                    for (int i = 0; i < N; ++i) b[t].p[i] = row_operand<AP>(sx + i * C * AP, row_at, 16 * t, 32 * s);
+                if (s + 1 < AP / 32) split_m(s + 1);
+                products<kOrder>([&](int i, int j) {           // (independent ones behind each other)
+#pragma unroll
+                    for (int c = 0; c < CT; ++c)
+#pragma unroll
+                        for (int t = 0; t < kTiles; ++t) o[t][c] = mfma(m[s & 1][c].p[i], b[t].p[j], o[t][c]);
+                }, m[0][0], b[0]);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        __syncthreads();                           // (X and Z have been read)
+        if (at + C < length) fetch(length - at - C, sy + (half ^ kDirectly) * C * AP);
+        if (reads) {
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                for (int c = 0; c < CT; ++c) o[t][c] *= reading[t];
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) {
+                Parts<N> b[kTiles];
+#pragma unroll
+                for (int t = 2 * s; t < kTiles; ++t)
+#pragma unroll
+                    for (int i = 0; i < N; ++i) b[t].p[i] = row_operand<C>(sp + i * C * C, p_at, 16 * t, 32 * s);
+                products<kOrder>([&](int i, int j) {
+#pragma unroll
+                    for (int t = 2 * s; t < kTiles; ++t)
+#pragma unroll
+                        for (int c = 0; c < CT; ++c) o[t][c] = mfma(zt[s][c].p[i], b[t].p[j], o[t][c]);
+                }, zt[0][0], b[0]);
+            }
+        { asm volatile("" ::: "memory"); __builtin_amdgcn_sched_barrier(0); unsigned long long now_ = __builtin_readcyclecounter(); if (reads) acc_[11] += now_ - last_; last_ = now_; __builtin_amdgcn_sched_barrier(0); }
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) {
+                if (16 * t + l >= n) continue;
+                char *to_row = out + 16 * t * out_step + out_lane;
+                if (W.wide) store_columns<float, WHOLE, 4 * CT>((float *)to_row, col, (int)W.E, o[t], W.by_read);
+                else store_columns<T, WHOLE, 4 * CT>((T *)to_row, col, (int)W.E, o[t], W.by_read);
+            }
+            out += C * out_step;
+        }
+        { asm volatile("" ::: "memory"); __builtin_amdgcn_sched_barrier(0); unsigned long long now_ = __builtin_readcyclecounter(); if (reads) acc_[8] += now_ - last_; last_ = now_; __builtin_amdgcn_sched_barrier(0); }
+        // the state
+        const Decay decay(log_decay, (float)n);
+        if (decay.slow)
+#pragma unroll
+            for (int t = 0; t < AP / 16; ++t)
+#pragma unroll
+                for (int c = 0; c < CT; ++c) M[t][c] = __builtin_elementwise_fma(M[t][c], f32x4{decay.by, decay.by, decay.by, decay.by}, M[t][c]);
+        else
+#pragma unroll
+            for (int t = 0; t < AP / 16; ++t)
+#pragma unroll
+                for (int c = 0; c < CT; ++c) M[t][c] *= decay.by;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+        { asm volatile("" ::: "memory"); __builtin_amdgcn_sched_barrier(0); unsigned long long now_ = __builtin_readcyclecounter(); if (reads) acc_[9] += now_ - last_; last_ = now_; __builtin_amdgcn_sched_barrier(0); }
+            __builtin_amdgcn_sched_barrier(0);
+            const f32x8 w = *(const f32x8 *)(weight + 32 * s + 8 * g);
+            Parts<3> wz[CT];
+#pragma unroll
+            for (int c = 0; c < CT; ++c) {
+                f32x8 v = __builtin_convertvector(zt[s][c].p[N - 1], f32x8);
+#pragma unroll
+                for (int m = N - 2; m >= 0; --m) v += __builtin_convertvector(zt[s][c].p[m], f32x8);
+                wz[c] = split<3>(v * w);
+            }
+#pragma unroll
+            for (int t = 0; t < AP / 16; t += 2) {
+                Parts<N> yt[2];
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int m = 0; m < N; ++m) yt[u].p[m] = column_operand<AP>(y_now + m * C * AP, y_at, 32 * s, 16 * t + 4 * u);
+                auto add = [&](int i, int j) {
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int c = 0; c < CT; ++c) M[t + u][c] = mfma(yt[u].p[i], wz[c].p[j], M[t + u][c]);
+                };
+                if (exact)
+#pragma unroll
+                    for (int i = 0; i < N; ++i) add(i, 2 - i);
+                products<2>(add, yt[0], Parts<2>());
+            }
+        }
+    }
+    const size_t m_a = reads ? W.m_a : W.E, m_e = reads ? W.m_e : 1;
+    each_of_state<AP, CT>(M, to != nullptr, e0 + wave_e, W.A, W.E, m_a, m_e, [&](float &m, size_t i) { to[i] = m; });
+}
+
+// What each segment of a row starts from, from what the segments in front of it add: a thread takes one element of the state along the row.
+constexpr int kJoinThreads = 256;
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(WalkArgs W)
+{
+    const unsigned size = W.A * W.E, blocks = (size + kJoinThreads - 1) / kJoinThreads;
+    const unsigned i = blockIdx.x % blocks * kJoinThreads + threadIdx.x, h = blockIdx.x / blocks % W.heads, r = blockIdx.x / blocks / W.heads;
+    if (i >= size) return;
+    long long lo, hi;
+    row_extent(W.offsets, r, W.total, lo, hi);
+    const long long segment = 1ll << W.segment_log2, segments = (hi - lo + segment - 1) >> W.segment_log2, first = (lo >> W.segment_log2) + r;
+    if (segments <= 1 || first + segments > (long long)W.pieces) return;
+    const long long slot = state_of(W.slots, r, W.states);
+    const unsigned a = i / W.E, e = i % W.E;
+    float m = W.m_in && slot >= 0 ? W.m_in[((size_t)slot * W.heads + h) * size + (size_t)a * W.m_a + (size_t)e * W.m_e] : 0.0f;
+    const Decay decay(W.log_decay[h], (float)segment);
+    float *p = W.between + ((size_t)first * W.heads + h) * size + i;
+    const size_t step = (size_t)W.heads * size;
+    for (long long s = 0; s + 1 < segments; ++s, p += step) {
+        const float added = *p;
+        *p = m;
+        m = decay(m) + added;
+    }
+    *p = m;
+}
+
+// out[t][stored head][i] = the sum of part[t][head][i] over the heads that share the stored head.
+struct SumArgs {
+    const float *part;
+    Heads out;
+    long long total;
+    unsigned heads, D;
+};
+constexpr int kSumThreads = 256;
+template <int DT> __global__ __launch_bounds__(kSumThreads) void sum_heads_kernel(SumArgs S)
+{
+    typedef typename Elem<DT>::T T;
+    const size_t i = (size_t)blockIdx.x * kSumThreads + threadIdx.x;
+    if (i >= (size_t)S.total * S.out.heads * S.D) return;
+    const unsigned d = (unsigned)(i % S.D), h = (unsigned)(i / S.D % S.out.heads), group = S.heads / S.out.heads;
+    const long long t = (long long)(i / S.D / S.out.heads);
+    const float *p = S.part + ((size_t)t * S.heads + (size_t)h * group) * S.D + d;
+    float sum = 0.0f;
+    for (unsigned g = 0; g < group; ++g) sum += p[(size_t)g * S.D];
+    ((T *)S.out.data)[t * S.out.token + (long long)h * S.out.head + d] = (T)sum;
+}
+
+// One token for each of many sequences.  A workgroup takes a block of columns of one state: 2^lanes_log2 lanes to a row, VEC columns each, as many rows at
+// a time as the workgroup has lanes for.  The state is read and written once; nothing else counts.
+struct StepArgs {
+    Heads q, k, v, out;
+    const float *log_decay;
+    const long long *slots;
+    float *state;
+    void *ws;
+    long long states;
+    unsigned n, heads, A, E, blocks, lanes_log2;
+    float scale;
+};
+constexpr int kStepThreads = 256;
+template <int DT, int VEC> __global__ __launch_bounds__(kStepThreads) void step_kernel(StepArgs S)
+{
+    typedef typename Elem<DT>::T T;
+    typedef float Vec __attribute__((ext_vector_type(VEC)));
+    __shared__ float ks[kMaxDim], qs[kMaxDim];
+    __shared__ Vec sums[kStepThreads / 64][64];
+    const unsigned block = blockIdx.x % S.blocks, h = blockIdx.x / S.blocks % S.heads, i = blockIdx.x / S.blocks / S.heads;
+    const unsigned lanes = 1u << S.lanes_log2, e = (block * lanes + (threadIdx.x & (lanes - 1))) * VEC, row0 = threadIdx.x >> S.lanes_log2, rows = kStepThreads >> S.lanes_log2;
+    const long long slot = state_of(S.slots, i, S.states);
+    if (threadIdx.x == 0 && block == 0 && h == 0 && S.slots && S.slots[i] >= S.states) raise_fault(S.ws, kFaultBadIndex);
+    const bool column = e < S.E, there = slot >= 0;
+    float *m = S.state + ((size_t)(there ? slot : 0) * S.heads + h) * S.A * S.E + e;
+    constexpr unsigned kAhead = 8;
+    Vec s[kAhead];
+    // the first rows are on their way before anything else is looked at
+    auto load = [&](unsigned a0) {
+#pragma unroll
+        for (unsigned u = 0; u < kAhead; ++u) {
+            const unsigned a = a0 + u * rows;
+            s[u] = Vec{};
+            if (there && column && a < S.A) s[u] = *(const Vec *)(m + (size_t)a * S.E);
+        }
+    };
+    load(row0);
+    const T *q = (const T *)S.q.data + S.q.at(h, S.heads) + i * S.q.token, *k = (const T *)S.k.data + S.k.at(h, S.heads) + i * S.k.token,
+            *v = (const T *)S.v.data + S.v.at(h, S.heads) + i * S.v.token;
+    for (unsigned a = threadIdx.x; a < S.A; a += kStepThreads) {
+        ks[a] = (float)k[a];
+        qs[a] = (float)q[a];
+    }
+    Vec ve = {}, sum = {};
+#pragma unroll
+    for (int c = 0; c < VEC; ++c)
+        if (e + c < S.E) ve[c] = (float)v[e + c];
+    const Decay decay(S.log_decay[h], 1.0f);
+    __syncthreads();
+    for (unsigned a0 = row0; a0 < S.A; a0 += kAhead * rows) {
+        if (a0 != row0) load(a0);
+#pragma unroll
+        for (unsigned u = 0; u < kAhead; ++u) {
+            const unsigned a = a0 + u * rows;
+            if (a >= S.A) break;
+#pragma unroll
+            for (int c = 0; c < VEC; ++c) {
+                s[u][c] = fmaf(ks[a], ve[c], decay(s[u][c]));
+                sum[c] = fmaf(qs[a], s[u][c], sum[c]);
+            }
+            if (there && column) *(Vec *)(m + (size_t)a * S.E) = s[u];
+        }
+    }
+    // over the rows: lanes of a wavefront that have the same columns, then the wavefronts
+#pragma unroll
+    for (int c = 0; c < VEC; ++c)
+        for (unsigned d = lanes; d < 64; d *= 2) sum[c] += __shfl_xor(sum[c], (int)d);
+    sums[threadIdx.x >> 6][threadIdx.x & 63] = sum;
+    __syncthreads();
+    if (threadIdx.x >= lanes || !column) return;
+#pragma unroll
+    for (int w = 1; w < kStepThreads / 64; ++w) sum += sums[w][threadIdx.x];
+    T *out = (T *)S.out.data + S.out.at(h, S.heads) + i * S.out.token;
+#pragma unroll
+    for (int c = 0; c < VEC; ++c)
+        if (e + c < S.E) out[e + c] = (T)(sum[c] * S.scale);
+}
+
+bool launch(const void *fn, size_t grid, unsigned block, void *args, hipStream_t s)
+{
+    void *list[] = {args};
+    return hipLaunchKernel(fn, dim3((unsigned)grid), dim3(block), list, 0, s) == hipSuccess;
+}
+
+template <template <int> class Pick> const void *pick(int dt) { return dt == kF16 ? Pick<kF16>::fn() : dt == kF32 ? Pick<kF32>::fn() : Pick<kBF16>::fn(); }
+template <int DT> struct SumHeads { static const void *fn() { return (const void *)sum_heads_kernel<DT>; } };
+template <int DT> struct Step { static const void *fn() { return (const void *)step_kernel<DT, 1>; } };
+template <int DT> struct StepByFour { static const void *fn() { return (const void *)step_kernel<DT, 4>; } };
+
+constexpr size_t kMostBlocks = 0x7FFFFFFFu;
+
+// What a call can do, by its sizes alone: TCUSCAN_OK, or why not.
+tcuscan_status_t check_shape(const tcuscan_attention_shape_t *p, int dt)
+{
+    if (!p) return TCUSCAN_ERR_INVALID_ARG;
+    const tcuscan_attention_shape_t &s = *p;
+    if (!elem_bytes(dt)) return TCUSCAN_ERR_UNSUPPORTED;
+    if (s.rows < 0 || s.total < 0 || s.heads < 1 || s.dk < 1 || s.dv < 1) return TCUSCAN_ERR_INVALID_ARG;
+    for (long long shared : {s.q_heads, s.k_heads, s.v_heads})
+        if (shared < 1 || shared > s.heads || s.heads % shared) return TCUSCAN_ERR_INVALID_ARG;
+    if (s.dk > kMaxDim || s.dv > kMaxDim) return TCUSCAN_ERR_UNSUPPORTED;
+    if (s.total >> 40) return TCUSCAN_ERR_UNSUPPORTED;
+    if (s.rows > 0x3FFFFFFF || s.heads > 0xFFFF || (unsigned long long)s.rows * s.heads > kMostBlocks / 8) return TCUSCAN_ERR_UNSUPPORTED;
+    return TCUSCAN_OK;
+}
+
+// Rows are cut into segments so that a call with few rows and heads still has a workgroup or two for every compute unit.
+constexpr size_t kWantedGroups = 512;
+constexpr unsigned kMinSegmentLog2 = 9, kWholeRows = 62;
+unsigned segment_log2_for(const tcuscan_attention_shape_t &s)
+{
+    const size_t blocks = (size_t)((s.dk > s.dv ? s.dk : s.dv) + 127) / 128;
+    unsigned log2 = kMinSegmentLog2;
+    while (((size_t)s.total * s.heads * blocks) >> log2 > kWantedGroups) ++log2;
+    return (size_t)s.total >> log2 ? log2 : kWholeRows;
+}
+size_t pieces_for(const tcuscan_attention_shape_t &s, unsigned segment_log2) { return (size_t)s.rows + ((size_t)s.total >> segment_log2); }
+
+struct Layout {
+    size_t between, part, all;
+    unsigned segment_log2;
+    Layout(const tcuscan_attention_shape_t &s, bool backward)
+    {
+        segment_log2 = segment_log2_for(s);
+        between = chain_layout::kHeaderBytes;
+        part = between + (segment_log2 == kWholeRows ? 0 : pieces_for(s, segment_log2) * s.heads * s.dk * s.dv * 4);
+        part = (part + 255) / 256 * 256;
+        size_t wide = 0;
+        if (backward) {
+            if (s.q_heads < s.heads || s.k_heads < s.heads) wide = (size_t)s.dk;
+            if (s.v_heads < s.heads && (size_t)s.dv > wide) wide = (size_t)s.dv;
+        }
+        all = part + (size_t)s.total * s.heads * wide * 4;
+    }
+};
+
+bool misaligned(const void *p, size_t to) { return (uintptr_t)p % to != 0; }
+
+Heads heads_of(const void *data, long long token, long long head, long long heads) { return {(void *)data, token, head, (unsigned)heads}; }
+
+template <int DT, int CT, bool WHOLE> const void *walk_for(unsigned A)
+{
+    return A <= 32 ? (const void *)walk_kernel<DT, 32, CT, WHOLE> : A <= 64 ? (const void *)walk_kernel<DT, 64, CT, WHOLE>
+         : A <= 128 ? (const void *)walk_kernel<DT, 128, CT, WHOLE> : (const void *)walk_kernel<DT, 256, 1, WHOLE>;
+}
+template <int CT, bool WHOLE> const void *walk_for(int dt, unsigned A)
+{
+    return dt == kF16 ? walk_for<kF16, CT, WHOLE>(A) : dt == kF32 ? walk_for<kF32, CT, WHOLE>(A) : walk_for<kBF16, CT, WHOLE>(A);
+}
+
+// Whether groups of eight elements of every token's features are aligned and whole, and 64 tokens within reach of a 32-bit offset.
+bool whole(const Heads &x, unsigned dims, size_t esz)
+{
+    return dims % 8 == 0 && (uintptr_t)x.data % 16 == 0 && (size_t)x.token * esz % 16 == 0 && (size_t)x.head * esz % 16 == 0 &&
+           (x.token < 0 ? -x.token : x.token) < (1ll << 22);
+}
+
+// One walk, into `out`; with heads that share the output, into `part` first.
+tcuscan_status_t walk(WalkArgs W, Heads out, float *part, int dt, hipStream_t s)
+{
+    const size_t esz = elem_bytes(dt);
+    const unsigned tiles = W.E <= 64 || W.A > 128 ? 1 : 2, cols = 64 * tiles;           // (256 rows of a state and 32 columns do not fit the registers)
+    const size_t groups = (size_t)W.pieces * W.heads * ((W.E + cols - 1) / cols);
+    const size_t join_groups = (size_t)W.rows * W.heads * (((size_t)W.A * W.E + kJoinThreads - 1) / kJoinThreads);
+    if (groups > kMostBlocks || join_groups > kMostBlocks) return TCUSCAN_ERR_UNSUPPORTED;
+    const bool shared = out.heads < W.heads;
+    const Heads to = shared ? Heads{part, (long long)W.heads * W.E, W.E, W.heads} : out;
+    W.wide = shared;
+    const bool all_whole = whole(W.x, W.A, esz) && whole(W.y, W.A, esz) && whole(W.z, W.E, esz) && whole(to, W.E, shared ? 4 : esz) && to.token > 0;
+    const void *fn = tiles == 1 ? all_whole ? walk_for<1, true>(dt, W.A) : walk_for<1, false>(dt, W.A)
+                                : all_whole ? walk_for<2, true>(dt, W.A) : walk_for<2, false>(dt, W.A);
+    if (W.segment_log2 != kWholeRows) {
+        W.out = Heads{};
+        if (!launch(fn, groups, 64 * kWalkWaves, &W, s) || !launch((const void *)join_kernel, join_groups, kJoinThreads, &W, s)) return TCUSCAN_ERR_HIP;
+    }
+    W.out = to;
+    if (!W.out.data) W.out.data = W.ws;            // (no tokens: nothing is written there)
+    if (!launch(fn, groups, 64 * kWalkWaves, &W, s)) return TCUSCAN_ERR_HIP;
+    const size_t items = (size_t)W.total * out.heads * W.E;
+    if (!shared || !items) return TCUSCAN_OK;
+    SumArgs S = {part, out, W.total, W.heads, W.E};
+    if ((items + kSumThreads - 1) / kSumThreads > kMostBlocks) return TCUSCAN_ERR_UNSUPPORTED;
+    return launch(pick<SumHeads>(dt), (items + kSumThreads - 1) / kSumThreads, kSumThreads, &S, s) ? TCUSCAN_OK : TCUSCAN_ERR_HIP;
+}
+
+}  // namespace
+
+extern "C" __attribute__((visibility("default"))) int prof_read(unsigned long long *h) { unsigned long long z[16] = {}; if (hipDeviceSynchronize() || hipMemcpyFromSymbol(h, HIP_SYMBOL(g_prof), 128) || hipMemcpyToSymbol(HIP_SYMBOL(g_prof), z, 128)) return 1; return 0; }
+extern "C" {
+
+size_t tcuscan_decay_attention_workspace_bytes(const tcuscan_attention_shape_t *shape, tcuscan_dtype_t dt, int backward)
+{
+    return check_shape(shape, dt) != TCUSCAN_OK ? 0 : Layout(*shape, backward != 0).all;
+}
+
+tcuscan_status_t tcuscan_decay_attention(const tcuscan_attention_shape_t *shape, const void *d_q, const void *d_k, const void *d_v, void *d_out,
+                                         const float *d_log_decay, const long long *d_offsets, tcuscan_dtype_t dt, float scale,
+                                         const float *d_state_in, float *d_state_out, const long long *d_slots, size_t states,
+                                         void *d_ws, size_t ws_bytes, tcuscan_stream_t stream)
+{
+    const tcuscan_status_t st = check_shape(shape, dt);
+    if (st != TCUSCAN_OK) return st;
+    const tcuscan_attention_shape_t &p = *shape;
+    if (p.rows == 0 || (p.total == 0 && !d_state_out)) return TCUSCAN_OK;
+    const size_t esz = elem_bytes(dt);
+    if (!d_log_decay || !d_offsets || misaligned(d_log_decay, 4) || misaligned(d_offsets, 8) || misaligned(d_slots, 8)) return TCUSCAN_ERR_INVALID_ARG;
+    if (misaligned(d_state_in, 16) || misaligned(d_state_out, 16)) return TCUSCAN_ERR_INVALID_ARG;
+    if (p.total && (!d_q || !d_k || !d_v || !d_out || misaligned(d_q, esz) || misaligned(d_k, esz) || misaligned(d_v, esz) || misaligned(d_out, esz)))
+        return TCUSCAN_ERR_INVALID_ARG;
+    if (p.total && (d_out == d_q || d_out == d_k || d_out == d_v)) return TCUSCAN_ERR_INVALID_ARG;
+    if (!d_slots && (d_state_in || d_state_out) && states < (size_t)p.rows) return TCUSCAN_ERR_INVALID_ARG;
+    const Layout L(p, false);
+    if (!d_ws || ws_bytes < L.all || misaligned(d_ws, 16)) return TCUSCAN_ERR_WORKSPACE;
+    WalkArgs W = {};
+    W.x = heads_of(d_q, p.q_token, p.q_head, p.q_heads);
+    W.y = heads_of(d_k, p.k_token, p.k_head, p.k_heads);
+    W.z = heads_of(d_v, p.v_token, p.v_head, p.v_heads);
+    W.log_decay = d_log_decay; W.offsets = d_offsets; W.slots = d_slots; W.m_in = d_state_in; W.m_out = d_state_out; W.ws = d_ws;
+    W.between = (float *)((char *)d_ws + L.between); W.segment_log2 = L.segment_log2; W.pieces = (unsigned)pieces_for(p, L.segment_log2);
+    W.states = (long long)states; W.total = p.total; W.rows = (unsigned)p.rows; W.heads = (unsigned)p.heads;
+    W.A = (unsigned)p.dk; W.E = (unsigned)p.dv; W.m_a = W.E; W.m_e = 1;
+    W.by_new = 1.0f; W.by_read = scale; W.from_end = 0;
+    return walk(W, heads_of(d_out, p.o_token, p.o_head, p.heads), nullptr, dt, (hipStream_t)stream);
+}
+
+tcuscan_status_t tcuscan_decay_attention_backward(const tcuscan_attention_shape_t *shape, const void *d_q, const void *d_k, const void *d_v, const void *d_out_grad,
+                                                  void *d_q_grad, void *d_k_grad, void *d_v_grad, const float *d_log_decay, const long long *d_offsets,
+                                                  tcuscan_dtype_t dt, float scale, const float *d_state_in, const float *d_state_out_grad,
+                                                  float *d_state_in_grad, void *d_ws, size_t ws_bytes, tcuscan_stream_t stream)
+{
+    const tcuscan_status_t st = check_shape(shape, dt);
+    if (st != TCUSCAN_OK) return st;
+    const tcuscan_attention_shape_t &p = *shape;
+    if (p.rows == 0 || (p.total == 0 && !d_state_in_grad)) return TCUSCAN_OK;
+    const size_t esz = elem_bytes(dt);
+    if (!d_log_decay || !d_offsets || misaligned(d_log_decay, 4) || misaligned(d_offsets, 8)) return TCUSCAN_ERR_INVALID_ARG;
+    if (misaligned(d_state_in, 16) || misaligned(d_state_out_grad, 16) || misaligned(d_state_in_grad, 16)) return TCUSCAN_ERR_INVALID_ARG;
+    const void *ins[] = {d_q, d_k, d_v, d_out_grad}, *outs[] = {d_q_grad, d_k_grad, d_v_grad};
+    if (p.total) {
+        for (const void *i : ins)
+            if (!i || misaligned(i, esz)) return TCUSCAN_ERR_INVALID_ARG;
+        for (const void *o : outs) {
+            if (!o || misaligned(o, esz)) return TCUSCAN_ERR_INVALID_ARG;
+            for (const void *i : ins)
+                if (o == i) return TCUSCAN_ERR_INVALID_ARG;
+        }
+        if (d_q_grad == d_k_grad || d_q_grad == d_v_grad || d_k_grad == d_v_grad) return TCUSCAN_ERR_INVALID_ARG;
+    }
+    if (d_state_in_grad && (d_state_in_grad == d_state_in || d_state_in_grad == d_state_out_grad)) return TCUSCAN_ERR_INVALID_ARG;
+    const Layout L(p, true);
+    if (!d_ws || ws_bytes < L.all || misaligned(d_ws, 16)) return TCUSCAN_ERR_WORKSPACE;
+    float *part = (float *)((char *)d_ws + L.part);
+    hipStream_t s = (hipStream_t)stream;
+    const Heads q = heads_of(d_q, p.q_token, p.q_head, p.q_heads), k = heads_of(d_k, p.k_token, p.k_head, p.k_heads),
+                v = heads_of(d_v, p.v_token, p.v_head, p.v_heads), o = heads_of(d_out_grad, p.o_token, p.o_head, p.heads);
+    WalkArgs W = {};
+    W.log_decay = d_log_decay; W.offsets = d_offsets; W.ws = d_ws;
+    W.between = (float *)((char *)d_ws + L.between); W.segment_log2 = L.segment_log2; W.pieces = (unsigned)pieces_for(p, L.segment_log2);
+    W.states = p.rows; W.total = p.total; W.rows = (unsigned)p.rows; W.heads = (unsigned)p.heads;
+    const unsigned dk = (unsigned)p.dk, dv = (unsigned)p.dv;
+    // dq, with the states of the forward pass
+    W.x = o; W.y = v; W.z = k; W.A = dv; W.E = dk; W.m_a = 1; W.m_e = dv; W.m_in = d_state_in;
+    W.by_new = 1.0f; W.by_read = scale; W.from_end = 0;
+    tcuscan_status_t r = walk(W, heads_of(d_q_grad, p.dq_token, p.dq_head, p.q_heads), part, dt, s);
+    if (r != TCUSCAN_OK) return r;
+    // dk, dv and the gradient by the first states, from the end
+    W.by_new = scale; W.by_read = 1.0f; W.from_end = 1; W.m_in = d_state_out_grad;
+    W.x = v; W.y = o; W.z = q;
+    r = walk(W, heads_of(d_k_grad, p.dk_token, p.dk_head, p.k_heads), part, dt, s);
+    if (r != TCUSCAN_OK) return r;
+    W.x = k; W.y = q; W.z = o; W.A = dk; W.E = dv; W.m_a = dv; W.m_e = 1; W.m_out = d_state_in_grad;
+    return walk(W, heads_of(d_v_grad, p.dv_token, p.dv_head, p.v_heads), part, dt, s);
+}
+
+tcuscan_status_t tcuscan_decay_attention_step(const tcuscan_attention_shape_t *shape, const void *d_q, const void *d_k, const void *d_v, void *d_out,
+                                              const float *d_log_decay, tcuscan_dtype_t dt, float scale, float *d_state, const long long *d_slots,
+                                              size_t states, void *d_ws, size_t ws_bytes, tcuscan_stream_t stream)
+{
+    const tcuscan_status_t st = check_shape(shape, dt);
+    if (st != TCUSCAN_OK) return st;
+    const tcuscan_attention_shape_t &p = *shape;
+    if (p.rows != p.total) return TCUSCAN_ERR_INVALID_ARG;
+    if (p.rows == 0) return TCUSCAN_OK;
+    const size_t esz = elem_bytes(dt);
+    if (!d_log_decay || !d_state || !d_q || !d_k || !d_v || !d_out) return TCUSCAN_ERR_INVALID_ARG;
+    if (misaligned(d_log_decay, 4) || misaligned(d_state, 16) || misaligned(d_slots, 8)) return TCUSCAN_ERR_INVALID_ARG;
+    if (misaligned(d_q, esz) || misaligned(d_k, esz) || misaligned(d_v, esz) || misaligned(d_out, esz)) return TCUSCAN_ERR_INVALID_ARG;
+    if (d_out == d_q || d_out == d_k || d_out == d_v || (!d_slots && states < (size_t)p.rows)) return TCUSCAN_ERR_INVALID_ARG;
+    if (d_ws && (ws_bytes < chain_layout::kHeaderBytes || misaligned(d_ws, 8))) return TCUSCAN_ERR_WORKSPACE;
+    StepArgs S = {};
+    S.q = heads_of(d_q, p.q_token, p.q_head, p.q_heads); S.k = heads_of(d_k, p.k_token, p.k_head, p.k_heads);
+    S.v = heads_of(d_v, p.v_token, p.v_head, p.v_heads); S.out = heads_of(d_out, p.o_token, p.o_head, p.heads);
+    S.log_decay = d_log_decay; S.slots = d_slots; S.state = d_state; S.ws = d_ws; S.states = (long long)states;
+    S.n = (unsigned)p.rows; S.heads = (unsigned)p.heads; S.A = (unsigned)p.dk; S.E = (unsigned)p.dv; S.scale = scale;
+    // lanes to a row: all of it, up to a wavefront; 128 bytes where there are few states, for more workgroups
+    const unsigned vec = S.E % 4 == 0 ? 4 : 1, row_lanes = (S.E + vec - 1) / vec;
+    const size_t all = (size_t)p.rows * p.heads;
+    while ((1u << S.lanes_log2) < row_lanes && S.lanes_log2 < 6) ++S.lanes_log2;
+    while (S.lanes_log2 > 3 && all * ((row_lanes + (1u << S.lanes_log2) - 1) >> S.lanes_log2) < kWantedGroups) --S.lanes_log2;
+    S.blocks = (row_lanes + (1u << S.lanes_log2) - 1) >> S.lanes_log2;
+    if (all * S.blocks > kMostBlocks) return TCUSCAN_ERR_UNSUPPORTED;
+    return launch(vec == 4 ? pick<StepByFour>(dt) : pick<Step>(dt), all * S.blocks, kStepThreads, &S, (hipStream_t)stream) ? TCUSCAN_OK : TCUSCAN_ERR_HIP;
+}
+
+}  // extern "C"

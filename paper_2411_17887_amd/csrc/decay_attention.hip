@@ -17,6 +17,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "../../include/tcuscan.h"
 #include "chain_layout.h"
 #include "element_types.h"
@@ -116,6 +118,7 @@ constexpr int parts_of(int dt) { return dt == kBF16 ? 1 : dt == kF16 ? 2 : 3; }
 constexpr int block_tokens(int dt, int ap) { return dt == kF32 || (dt == kF16 && ap > 128) ? 32 : 64; }
 
 constexpr int kWalkWaves = 4;
+constexpr int kLoadsDone = 0x0F70;                 // s_waitcnt: no load or store on its way, whatever else is
 // Workgroups on a compute unit, by what LDS and registers give.
 constexpr int groups_at_once(int dt, int ap, int ct) { return ap > 128 || (dt != kBF16 && ap > 64) || (dt == kF16 && ct > 1) ? 1 : 2; }
 
@@ -186,36 +189,64 @@ __device__ __forceinline__ int here(int v)
     return v;
 }
 
-// A block of tokens on its way from memory to LDS: C rows of COLS elements, eight at a time, spread over THREADS lanes.  WHOLE: granules of eight
-// elements are aligned and either inside or outside; they wait in registers while the block before is worked on.  Otherwise the block is
-// read element by element when its turn comes.
+// A block of tokens on its way from memory to LDS: C rows of COLS elements, a granule of eight to a lane at a time.  Rows from n on and columns from `cols`
+// on become zeros.  Three ways:
+//   kDirect   bf16, granules aligned and either inside or outside: loads that write LDS themselves, lane after lane, so that it is the lanes' addresses
+//             that are permuted; what is outside is beyond the end of the buffer they read from.  They need no registers while they are on
+//             their way (held there, the 48 a lane would need at dk = dv = 128 are spilled).
+//   kStaged   fp32 and f16, granules as above: through registers, split into parts on the way.
+//   kSlow     anything else: element by element.
+enum Way { kDirect, kStaged, kSlow };
+constexpr Way way_of(int dt, bool whole) { return !whole ? kSlow : dt == kBF16 ? kDirect : kStaged; }
 template <int DT, int C, int COLS, int THREADS, bool WHOLE> struct Stage {
     typedef typename Elem<DT>::T T;
+    static constexpr Way kWay = way_of(DT, WHOLE);
     static constexpr int kItems = C * COLS / 8, kEach = (kItems + THREADS - 1) / THREADS, kQuads = sizeof(T) / 2, N = parts_of(DT);
     static constexpr int kRowsAtOnce = THREADS / (COLS / 8);
     static_assert(THREADS % (COLS / 8) == 0, "a lane keeps to its columns");
-    u32x4 v[WHOLE ? kEach : 1][kQuads];
-    const T *mine;                                 // the lane's first granule in the block
+    static constexpr int kOffsets = kRowsAtOnce % 16 == 0 ? 1 : 2;             // the swizzle repeats every 16 rows
+    static_assert(kRowsAtOnce % 8 == 0, "or every second time");
+    u32x4 v[kWay == kStaged ? kEach : 1][kQuads];
+    const T *first;                                // the block's first row (the same for all lanes)
     long long step;                                // from row to row
     int row, col, cols;
+    int offset[kOffsets];                          // kDirect: the lane's first granules in a whole block, in bytes from its lowest address
 
     __device__ __forceinline__ void begin(const T *p, long long row_step, int columns)
     {
-        row = (int)threadIdx.x / (COLS / 8); col = (int)threadIdx.x % (COLS / 8) * 8; cols = columns; step = row_step;
-        mine = p + row * step + col;
+        row = (int)threadIdx.x / (COLS / 8); col = (int)threadIdx.x % (COLS / 8) * 8; cols = columns; first = p; step = row_step;
+        if constexpr (kWay == kDirect)
+#pragma unroll
+            for (int i = 0; i < kOffsets; ++i) {
+                const int r = row + i * kRowsAtOnce, c = (int)(threadIdx.x % (COLS / 8) ^ Tile<COLS>::swizzle(r)) * 8;
+                offset[i] = c < cols ? ((step < 0 ? C - 1 - r : r) * (int)(step < 0 ? -step : step) + c) * (int)sizeof(T) : kOutside;
+            }
     }
-    // Rows from n on and columns from `cols` on are zeros.
-    __device__ __forceinline__ void load(int n)
+    static constexpr int kOutside = 1 << 30;       // beyond the end of any block (64 rows less than 2^22 elements apart)
+    // kDirect: all the way, to be waited for; kStaged: as far as the registers.
+    __device__ __forceinline__ void load(bf16_t *tile, int n)
     {
-        if constexpr (!WHOLE) return;
-        const T *p = mine;
+        if constexpr (kWay == kDirect) {
+            const int by_row = (int)(step < 0 ? -step : step) * (int)sizeof(T), shift = step < 0 ? (C - n) * by_row : 0;
+            const __amdgpu_buffer_rsrc_t block = __builtin_amdgcn_make_buffer_rsrc((void *)(step < 0 ? first + (n - 1) * step : first), 0, (n - 1) * by_row + cols * (int)sizeof(T), 0x00027000);
+            bf16_t *to = tile + __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64) * 512;
 #pragma unroll
-        for (int i = 0; i < kEach; ++i, p += kRowsAtOnce * step) {
+            for (int i = 0; i < kEach; ++i) {
+                const int at = offset[i % kOffsets] + (i - i % kOffsets) * kRowsAtOnce * (step < 0 ? -by_row : by_row) - shift;
+                if (kEach * THREADS <= kItems || (int)threadIdx.x < kItems)
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(block, (__attribute__((address_space(3))) void *)(to + i * THREADS * 8), 16, at, 0, 0, 0);
+            }
+            first += C * step;
+        } else if constexpr (kWay == kStaged) {
+            const T *p = first + row * step + col;
 #pragma unroll
-            for (int q = 0; q < kQuads; ++q) v[i][q] = u32x4{0u, 0u, 0u, 0u};
-            if (row + i * kRowsAtOnce < n && col < cols)
+            for (int i = 0; i < kEach; ++i, p += kRowsAtOnce * step) {
 #pragma unroll
-                for (int q = 0; q < kQuads; ++q) v[i][q] = ((const u32x4 *)p)[q];
+                for (int q = 0; q < kQuads; ++q) v[i][q] = u32x4{0u, 0u, 0u, 0u};
+                if (row + i * kRowsAtOnce < n && col < cols)
+#pragma unroll
+                    for (int q = 0; q < kQuads; ++q) v[i][q] = ((const u32x4 *)p)[q];
+            }
         }
     }
     static __device__ __forceinline__ void put(bf16_t *to, const T (&e)[8])                       // the parts are C * COLS elements apart
@@ -231,27 +262,27 @@ template <int DT, int C, int COLS, int THREADS, bool WHOLE> struct Stage {
             for (int n = 0; n < N; ++n) *(bf16x8 *)(to + n * C * COLS) = parts.p[n];
         }
     }
-    // (and on to the next block)
+    // kStaged and kSlow: the rest of the way, and on to the next block.
     __device__ __forceinline__ void store(bf16_t *tile, int n)
     {
-        if constexpr (WHOLE) {
+        if constexpr (kWay == kStaged) {
 #pragma unroll
             for (int i = 0; i < kEach; ++i) {
                 T e[8];
                 __builtin_memcpy(e, &v[i][0], sizeof e);
                 if (row + i * kRowsAtOnce < C) put(tile + Tile<COLS>::at(row + i * kRowsAtOnce, col), e);
             }
-        } else {
+        } else if constexpr (kWay == kSlow) {
 #pragma unroll 1
             for (int r = row; r < C; r += kRowsAtOnce) {
-                const T *p = mine + (r - row) * step;
+                const T *p = first + r * step + col;
                 T e[8];
 #pragma unroll
                 for (int k = 0; k < 8; ++k) e[k] = r < n && col + k < cols ? p[k] : (T)0.0f;
                 put(tile + Tile<COLS>::at(r, col), e);
             }
         }
-        mine += C * step;
+        first += C * step;
     }
 };
 
@@ -263,6 +294,10 @@ struct Piece {
     long long first, end;                          // the segment's, counted from where the walk starts
     bool last;
 };
+__device__ __forceinline__ long long uniform(long long v)
+{   // (the same in all lanes: into scalar registers)
+    return (long long)((unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)v));
+}
 __device__ __forceinline__ bool find_piece(const WalkArgs &W, unsigned number, Piece &p)
 {
     unsigned lo = 0, hi = W.rows;
@@ -277,6 +312,7 @@ __device__ __forceinline__ bool find_piece(const WalkArgs &W, unsigned number, P
     }
     p.r = lo;
     row_extent(W.offsets, p.r, W.total, p.lo, p.hi);
+    p.lo = uniform(p.lo); p.hi = uniform(p.hi);
     const long long length = p.hi - p.lo, s = one ? 0 : (long long)number - (p.lo >> W.segment_log2) - p.r, segment = 1ll << W.segment_log2;
     p.first = s * segment;
     if (s < 0 || (s > 0 && p.first >= length)) return false;
@@ -285,16 +321,19 @@ __device__ __forceinline__ bool find_piece(const WalkArgs &W, unsigned number, P
     return true;
 }
 
-// Four consecutive columns of the output, `col` the first of them.  WHOLE: they are aligned and all inside or all outside.
-template <class T, bool WHOLE> __device__ __forceinline__ void store_four(T *p, int col, int cols, f32x4 v)
+// K consecutive columns of the output, `col` the first of them.  WHOLE: they are aligned and all inside or all outside.
+template <class T, bool WHOLE, int K> __device__ __forceinline__ void store_columns(T *p, int col, int cols, const f32x4 *v, float by)
 {
-    typedef T T4 __attribute__((ext_vector_type(4)));
+    typedef T Some __attribute__((ext_vector_type(K)));
+    Some x;
+#pragma unroll
+    for (int k = 0; k < K; ++k) x[k] = (T)(v[k / 4][k % 4] * by);
     if constexpr (WHOLE) {
-        if (col < cols) *(T4 *)p = __builtin_convertvector(v, T4);
+        if (col < cols) *(Some *)p = x;
     } else {
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-            if (col + r < cols) p[r] = (T)v[r];
+        for (int k = 0; k < K; ++k)
+            if (col + k < cols) p[k] = x[k];
     }
 }
 
@@ -306,14 +345,14 @@ template <int AP, int CT, class What> __device__ __forceinline__ void each_of_st
     unsigned lane = threadIdx.x & 63;
     asm volatile("" : "+v"(lane));
     if (!any) return;
-    const unsigned a0 = 8 * (lane >> 4), e_lane = first_e + (lane & 15);
+    const unsigned a0 = 8 * (lane >> 4), e_lane = first_e + 4 * CT * ((lane & 15) >> 2) + (lane & 3);
 #pragma unroll
     for (int t = 0; t < AP / 16; ++t)
 #pragma unroll
         for (int c = 0; c < CT; ++c)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const unsigned a = a0 + 32 * (t / 2) + 4 * (t & 1) + r, e = e_lane + 16 * c;
+                const unsigned a = a0 + 32 * (t / 2) + 4 * (t & 1) + r, e = e_lane + 4 * c;
                 float m = M[t][c][r];
                 if (a < A && e < E) what(m, a * m_a + e * m_e);
                 M[t][c][r] = m;
@@ -324,8 +363,9 @@ template <int DT, int AP, int CT, bool WHOLE> __global__ __launch_bounds__(64 * 
 {
     typedef typename Elem<DT>::T T;
     constexpr int N = parts_of(DT), C = block_tokens(DT, AP), EB = 16 * kWalkWaves * CT, kThreads = 64 * kWalkWaves;
+    constexpr bool kDirectly = way_of(DT, WHOLE) == kDirect;
     constexpr int kTiles = C / 16, kSteps = C / 32, kOrder = N == 3 ? 3 : 2;       // tiles of 16 tokens, steps of 32
-    __shared__ __attribute__((aligned(16))) bf16_t sx[N * C * AP], sy[N * C * AP], sz[N * C * EB], sp[N * C * C];
+    __shared__ __attribute__((aligned(16))) bf16_t sx[N * C * AP], sy[(kDirectly ? 2 : 1) * N * C * AP], sz[N * C * EB], sp[N * C * C];
     __shared__ __attribute__((aligned(16))) float weight[C];
 
     const unsigned blocks = (W.E + EB - 1) / EB;
@@ -347,7 +387,8 @@ template <int DT, int AP, int CT, bool WHOLE> __global__ __launch_bounds__(64 * 
     const long long slot = state_of(W.slots, piece.r, W.states);
     const size_t state = ((size_t)slot * W.heads + h) * W.A * W.E, between = ((size_t)number * W.heads + h) * W.A * W.E;
     const bool cut = piece.first > 0 || !piece.last;                // a row of several segments
-    // M[2 s + t][c][r] is M[a][e] with a = 32 s + 8 g + 4 t + r, e = e0 + wave_e + 16 c + l
+    // M[2 s + t][c][r] is M[a][e] with a = 32 s + 8 g + 4 t + r, e = e0 + wave_e + 4 CT (l / 4) + 4 c + l % 4: the columns of a lane's outputs are
+    // then next to each other
     f32x4 M[AP / 16][CT] = {};
     {
         // a row of several segments finds what it starts from in the workspace, also for the first of them
@@ -370,56 +411,78 @@ template <int DT, int AP, int CT, bool WHOLE> __global__ __launch_bounds__(64 * 
     next_x.begin((const T *)W.x.data + W.x.at(h, W.heads) + origin * W.x.token, sign * W.x.token, (int)W.A);
     next_y.begin((const T *)W.y.data + W.y.at(h, W.heads) + origin * W.y.token, sign * W.y.token, (int)W.A);
     next_z.begin((const T *)W.z.data + W.z.at(h, W.heads) + origin * W.z.token + e0, sign * W.z.token, (int)W.E - e0);
-    // the lane's first output: token l of the block, column 4 g of the wavefront's
-    const int out_size = W.wide ? 4 : (int)sizeof(T);
-    char *out = (char *)W.out.data + (W.out.at(h, W.heads) + (origin + sign * l) * W.out.token + e0 + wave_e + 4 * g) * out_size;
-    const long long out_step = sign * 16 * W.out.token * out_size;
+    // the lane's first output: token l of the block, column 4 CT g of the wavefront's
+    const int out_size = W.wide ? 4 : (int)sizeof(T), col = e0 + wave_e + 4 * CT * g;
+    const long long out_step = sign * W.out.token * out_size;
+    char *out = (char *)W.out.data + (W.out.at(h, W.heads) + origin * W.out.token) * out_size + (sign < 0 ? 15 * out_step : 0);
+    typedef std::conditional_t<WHOLE, unsigned, long long> Offset;
+    const Offset out_lane = (Offset)((sign < 0 ? l - 15 : l) * out_step) + (Offset)(col * out_size);         // (not negative: outputs have positive strides)
     float *to = !reads ? W.between + between : piece.last && W.m_out && slot >= 0 ? W.m_out + state : nullptr;
     // the third part of what is added to a state counts where the state itself is asked for, not where 16-bit outputs are read from it
     const bool exact = to || DT == kF32;
     const long long length = piece.end - piece.first;
-    auto fetch = [&](long long left) {
+    // the next block: Y has two tiles in LDS if loads write there themselves, X and Z have been read before these start
+    auto fetch = [&](long long left, bf16_t *y_tile) {
         const int n = (int)(left < C ? left : C);
-        if (reads) next_x.load(n);
-        next_y.load(n);
-        next_z.load(n);
+        if (reads) next_x.load(sx, n);
+        next_y.load(y_tile, n);
+        next_z.load(sz, n);
     };
-    if (length > 0) fetch(length);
-    for (long long at = 0; at < length; at += C) {
-        const int n = (int)(length - at < C ? length - at : C);
-        const int row_at = here(row_lane<AP>(lane)), p_at = here(row_lane<C>(lane)), y_at = here(column_lane<AP, 8>(lane, 0)), z_at = here(column_lane<EB, 4>(lane, wave_e));
-        if (reads) next_x.store(sx, n);
-        next_y.store(sy, n);
-        next_z.store(sz, n);
+    auto write_weights = [&](int n) {
         if ((int)threadIdx.x < C)
             weight[threadIdx.x] = (int)threadIdx.x < n ? W.by_new * decay_power(log_decay, (float)(n - 1 - (int)threadIdx.x + (W.from_end ? 1 : 0))) : 0.0f;
+    };
+    if (length > 0) fetch(length, sy);
+    write_weights((int)(length < C ? length : C));
+    int half = 0;                                  // the tile of Y in use
+    for (long long at = 0; at < length; at += C, half ^= kDirectly) {
+        const int n = (int)(length - at < C ? length - at : C);
+        bf16_t *const y_now = sy + half * C * AP;
+        const int row_at = here(row_lane<AP>(lane)), p_at = here(row_lane<C>(lane)), y_at = here(column_lane<AP, 8>(lane, 0)), z_at = here(column_lane<EB, 4 * CT>(lane, wave_e));
+        if constexpr (kDirectly) {
+            __builtin_amdgcn_s_waitcnt(kLoadsDone);
+        } else {
+            __syncthreads();                       // everybody has done with the block before
+            if (reads) next_x.store(sx, n);
+            next_y.store(sy, n);
+            next_z.store(sz, n);
+        }
         __syncthreads();
+        if (n < C && at > 0) write_weights(n);     // (everybody has done with the block before, and reads them behind the next barrier)
         if (reads) {
-            // P^T, 16 keys by 16 queries at a time
+            // P^T, 16 keys by 16 queries at a time: the wavefronts take every fourth of the tiles on and below the diagonal, each all of its own at once
+            constexpr int kPTiles = kTiles * (kTiles + 1) / 2, kMine = (kPTiles + kWalkWaves - 1) / kWalkWaves;
+            int it[kMine], jt[kMine];
+            f32x4 p[kMine];
 #pragma unroll
-            for (int k = 0; k < (kTiles * (kTiles + 1) / 2 + kWalkWaves - 1) / kWalkWaves; ++k) {
-                const int tile = wave + k * kWalkWaves;
-                if (tile >= kTiles * (kTiles + 1) / 2) break;
-                const int it = tile >= 6 ? 3 : tile >= 3 ? 2 : tile >= 1 ? 1 : 0, jt = tile - it * (it + 1) / 2;
-                f32x4 p = {0.0f, 0.0f, 0.0f, 0.0f};
+            for (int k = 0; k < kMine; ++k) {
+                const int tile = min(wave + k * kWalkWaves, kPTiles - 1);
+                it[k] = tile >= 6 ? 3 : tile >= 3 ? 2 : tile >= 1 ? 1 : 0;
+                jt[k] = tile - it[k] * (it[k] + 1) / 2;
+                p[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            }
 #pragma unroll
-                for (int s = 0; s < AP / 32; ++s) {
+            for (int s = 0; s < AP / 32; ++s)
+#pragma unroll
+                for (int k = 0; k < kMine; ++k) {
                     Parts<N> a, b;
 #pragma unroll
                     for (int m = 0; m < N; ++m) {
-                        a.p[m] = row_operand<AP>(sy + m * C * AP, row_at, 16 * jt, 32 * s);
-                        b.p[m] = row_operand<AP>(sx + m * C * AP, row_at, 16 * it, 32 * s);
+                        a.p[m] = row_operand<AP>(y_now + m * C * AP, row_at, 16 * jt[k], 32 * s);
+                        b.p[m] = row_operand<AP>(sx + m * C * AP, row_at, 16 * it[k], 32 * s);
                     }
-                    products<kOrder>([&](int i, int j) { p = mfma(a.p[i], b.p[j], p); }, a, b);
+                    products<kOrder>([&](int i, int j) { p[k] = mfma(a.p[i], b.p[j], p[k]); }, a, b);
                 }
-                const int i = 16 * it + l, j = 16 * jt + 4 * g, apart = here(i - j);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) p[r] = apart >= r ? p[r] * (W.by_new * decay_power(log_decay, (float)(apart - r))) : 0.0f;
+            for (int k = 0; k < kMine; ++k) {
+                const int i = 16 * it[k] + l, j = 16 * jt[k] + 4 * g, apart = here(i - j);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) p[k][r] = apart >= r ? p[k][r] * (W.by_new * decay_power(log_decay, (float)(apart - r))) : 0.0f;
 #pragma unroll
                 for (int m = 0; m < N; ++m) {
-                    const bf16x4 part = __builtin_convertvector(p, bf16x4);
-                    *(bf16x4 *)(sp + m * C * C + Tile<C>::at(i, j)) = part;
-                    p -= __builtin_convertvector(part, f32x4);
+                    const bf16x4 part = __builtin_convertvector(p[k], bf16x4);
+                    if (wave + k * kWalkWaves < kPTiles) *(bf16x4 *)(sp + m * C * C + Tile<C>::at(i, j)) = part;
+                    p[k] -= __builtin_convertvector(part, f32x4);
                 }
             }
             __syncthreads();
@@ -430,14 +493,20 @@ template <int DT, int AP, int CT, bool WHOLE> __global__ __launch_bounds__(64 * 
 #pragma unroll
             for (int c = 0; c < CT; ++c)
 #pragma unroll
-                for (int m = 0; m < N; ++m) zt[s][c].p[m] = column_operand<EB>(sz + m * C * EB, z_at, 32 * s, 16 * c);
+                for (int m = 0; m < N; ++m) zt[s][c].p[m] = column_operand<EB>(sz + m * C * EB, z_at, 32 * s, 4 * c);
+        constexpr int NM = N == 3 ? 3 : 2;
+        f32x4 o[kTiles][CT];
         if (reads) {
-            constexpr int NM = N == 3 ? 3 : 2;
-            f32x4 o[kTiles][CT];
 #pragma unroll
             for (int t = 0; t < kTiles; ++t)
 #pragma unroll
                 for (int c = 0; c < CT; ++c) o[t][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            Parts<NM> m[2][CT];                    // this step's parts of M and the next one's
+            auto split_m = [&](int s) {
+#pragma unroll
+                for (int c = 0; c < CT; ++c) m[s & 1][c] = split<NM>(__builtin_shufflevector(M[2 * s][c], M[2 * s + 1][c], 0, 1, 2, 3, 4, 5, 6, 7));
+            };
+            split_m(0);
 #pragma unroll
             for (int s = 0; s < AP / 32; ++s) {
                 __builtin_amdgcn_sched_barrier(0);             // (or the parts of all steps take registers at once)
@@ -446,17 +515,19 @@ template <int DT, int AP, int CT, bool WHOLE> __global__ __launch_bounds__(64 * 
                 for (int t = 0; t < kTiles; ++t)
 #pragma unroll
                     for (int i = 0; i < N; ++i) b[t].p[i] = row_operand<AP>(sx + i * C * AP, row_at, 16 * t, 32 * s);
-                Parts<NM> m[CT];
-#pragma unroll
-                for (int c = 0; c < CT; ++c) m[c] = split<NM>(__builtin_shufflevector(M[2 * s][c], M[2 * s + 1][c], 0, 1, 2, 3, 4, 5, 6, 7));
+                if (s + 1 < AP / 32) split_m(s + 1);
                 products<kOrder>([&](int i, int j) {           // (independent ones behind each other)
 #pragma unroll
                     for (int c = 0; c < CT; ++c)
 #pragma unroll
-                        for (int t = 0; t < kTiles; ++t) o[t][c] = mfma(m[c].p[i], b[t].p[j], o[t][c]);
-                }, m[0], b[0]);
+                        for (int t = 0; t < kTiles; ++t) o[t][c] = mfma(m[s & 1][c].p[i], b[t].p[j], o[t][c]);
+                }, m[0][0], b[0]);
             }
-            __builtin_amdgcn_sched_barrier(0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        __syncthreads();                           // (X and Z have been read)
+        if (at + C < length) fetch(length - at - C, sy + (half ^ kDirectly) * C * AP);
+        if (reads) {
 #pragma unroll
             for (int t = 0; t < kTiles; ++t)
 #pragma unroll
@@ -476,19 +547,14 @@ template <int DT, int AP, int CT, bool WHOLE> __global__ __launch_bounds__(64 * 
                 }, zt[0][0], b[0]);
             }
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t, out += out_step) {
+            for (int t = 0; t < kTiles; ++t) {
                 if (16 * t + l >= n) continue;
-#pragma unroll
-                for (int c = 0; c < CT; ++c) {
-                    const int col = e0 + wave_e + 16 * c + 4 * g;
-                    const f32x4 v = o[t][c] * W.by_read;
-                    if (W.wide) store_four<float, WHOLE>((float *)out + 16 * c, col, (int)W.E, v);
-                    else store_four<T, WHOLE>((T *)out + 16 * c, col, (int)W.E, v);
-                }
+                char *to_row = out + 16 * t * out_step + out_lane;
+                if (W.wide) store_columns<float, WHOLE, 4 * CT>((float *)to_row, col, (int)W.E, o[t], W.by_read);
+                else store_columns<T, WHOLE, 4 * CT>((T *)to_row, col, (int)W.E, o[t], W.by_read);
             }
+            out += C * out_step;
         }
-        __builtin_amdgcn_sched_barrier(0);
-        if (at + C < length) fetch(length - at - C);
         // the state
         const Decay decay(log_decay, (float)n);
         if (decay.slow)
@@ -519,7 +585,7 @@ template <int DT, int AP, int CT, bool WHOLE> __global__ __launch_bounds__(64 * 
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
 #pragma unroll
-                    for (int m = 0; m < N; ++m) yt[u].p[m] = column_operand<AP>(sy + m * C * AP, y_at, 32 * s, 16 * t + 4 * u);
+                    for (int m = 0; m < N; ++m) yt[u].p[m] = column_operand<AP>(y_now + m * C * AP, y_at, 32 * s, 16 * t + 4 * u);
                 auto add = [&](int i, int j) {
 #pragma unroll
                     for (int u = 0; u < 2; ++u)
@@ -532,7 +598,6 @@ template <int DT, int AP, int CT, bool WHOLE> __global__ __launch_bounds__(64 * 
                 products<2>(add, yt[0], Parts<2>());
             }
         }
-        __syncthreads();
     }
     const size_t m_a = reads ? W.m_a : W.E, m_e = reads ? W.m_e : 1;
     each_of_state<AP, CT>(M, to != nullptr, e0 + wave_e, W.A, W.E, m_a, m_e, [&](float &m, size_t i) { to[i] = m; });
@@ -727,32 +792,32 @@ Heads heads_of(const void *data, long long token, long long head, long long head
 template <int DT, int CT, bool WHOLE> const void *walk_for(unsigned A)
 {
     return A <= 32 ? (const void *)walk_kernel<DT, 32, CT, WHOLE> : A <= 64 ? (const void *)walk_kernel<DT, 64, CT, WHOLE>
-         : A <= 128 ? (const void *)walk_kernel<DT, 128, CT, WHOLE> : (const void *)walk_kernel<DT, 256, CT, WHOLE>;
+         : A <= 128 ? (const void *)walk_kernel<DT, 128, CT, WHOLE> : (const void *)walk_kernel<DT, 256, 1, WHOLE>;
 }
 template <int CT, bool WHOLE> const void *walk_for(int dt, unsigned A)
 {
     return dt == kF16 ? walk_for<kF16, CT, WHOLE>(A) : dt == kF32 ? walk_for<kF32, CT, WHOLE>(A) : walk_for<kBF16, CT, WHOLE>(A);
 }
 
-// Whether groups of `n` elements of every token's features are aligned and whole.
-bool whole(const Heads &x, unsigned dims, size_t esz, unsigned n)
+// Whether groups of eight elements of every token's features are aligned and whole, and 64 tokens within reach of a 32-bit offset.
+bool whole(const Heads &x, unsigned dims, size_t esz)
 {
-    const size_t bytes = n * esz < 16 ? n * esz : 16;
-    return dims % n == 0 && (uintptr_t)x.data % bytes == 0 && (size_t)x.token * esz % bytes == 0 && (size_t)x.head * esz % bytes == 0;
+    return dims % 8 == 0 && (uintptr_t)x.data % 16 == 0 && (size_t)x.token * esz % 16 == 0 && (size_t)x.head * esz % 16 == 0 &&
+           (x.token < 0 ? -x.token : x.token) < (1ll << 22);
 }
 
 // One walk, into `out`; with heads that share the output, into `part` first.
 tcuscan_status_t walk(WalkArgs W, Heads out, float *part, int dt, hipStream_t s)
 {
     const size_t esz = elem_bytes(dt);
-    const unsigned tiles = W.E <= 64 ? 1 : 2, cols = 64 * tiles;
+    const unsigned tiles = W.E <= 64 || W.A > 128 ? 1 : 2, cols = 64 * tiles;           // (256 rows of a state and 32 columns do not fit the registers)
     const size_t groups = (size_t)W.pieces * W.heads * ((W.E + cols - 1) / cols);
     const size_t join_groups = (size_t)W.rows * W.heads * (((size_t)W.A * W.E + kJoinThreads - 1) / kJoinThreads);
     if (groups > kMostBlocks || join_groups > kMostBlocks) return TCUSCAN_ERR_UNSUPPORTED;
     const bool shared = out.heads < W.heads;
     const Heads to = shared ? Heads{part, (long long)W.heads * W.E, W.E, W.heads} : out;
     W.wide = shared;
-    const bool all_whole = whole(W.x, W.A, esz, 8) && whole(W.y, W.A, esz, 8) && whole(W.z, W.E, esz, 8) && whole(to, W.E, shared ? 4 : esz, 4);
+    const bool all_whole = whole(W.x, W.A, esz) && whole(W.y, W.A, esz) && whole(W.z, W.E, esz) && whole(to, W.E, shared ? 4 : esz) && to.token > 0;
     const void *fn = tiles == 1 ? all_whole ? walk_for<1, true>(dt, W.A) : walk_for<1, false>(dt, W.A)
                                 : all_whole ? walk_for<2, true>(dt, W.A) : walk_for<2, false>(dt, W.A);
     if (W.segment_log2 != kWholeRows) {
