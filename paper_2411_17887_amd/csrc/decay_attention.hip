@@ -365,8 +365,8 @@ template <int DT, int AP, int CT, bool WHOLE> __global__ __launch_bounds__(64 * 
     constexpr int N = parts_of(DT), C = block_tokens(DT, AP), EB = 16 * kWalkWaves * CT, kThreads = 64 * kWalkWaves;
     constexpr bool kDirectly = way_of(DT, WHOLE) == kDirect;
     constexpr int kTiles = C / 16, kSteps = C / 32, kOrder = N == 3 ? 3 : 2;       // tiles of 16 tokens, steps of 32
-    __shared__ __attribute__((aligned(16))) bf16_t sx[N * C * AP], sy[(kDirectly ? 2 : 1) * N * C * AP], sz[N * C * EB], sp[N * C * C];
-    __shared__ __attribute__((aligned(16))) float weight[C];
+    __shared__ __attribute__((aligned(16))) bf16_t sx[N * C * AP], sy[N * C * AP], sz[N * C * EB], sp[N * C * C];
+    __shared__ __attribute__((aligned(16))) bf16_t sy_too[kDirectly ? C * AP : 8];           // (an array of its own: loads into the one are not waited for to read the other)
 
     const unsigned blocks = (W.E + EB - 1) / EB;
     const unsigned block = blockIdx.x % blocks, h = blockIdx.x / blocks % W.heads, number = blockIdx.x / blocks / W.heads;
@@ -421,23 +421,30 @@ template <int DT, int AP, int CT, bool WHOLE> __global__ __launch_bounds__(64 * 
     // the third part of what is added to a state counts where the state itself is asked for, not where 16-bit outputs are read from it
     const bool exact = to || DT == kF32;
     const long long length = piece.end - piece.first;
-    // the next block: Y has two tiles in LDS if loads write there themselves, X and Z have been read before these start
-    auto fetch = [&](long long left, bf16_t *y_tile) {
-        const int n = (int)(left < C ? left : C);
-        if (reads) next_x.load(sx, n);
-        next_y.load(y_tile, n);
-        next_z.load(sz, n);
+    // Loads of the next block start where their tiles in LDS have been read (Y has two) and a part of the work at a time: more of them at once than
+    // the memory pipeline takes hold up the wavefront.
+    auto tokens = [&](long long left) { return (int)(left < C ? left : C); };
+    f32x8 weight[kSteps];                          // by_new a^(n-1-j), from the end a^(n-j), of the lane's tokens j of each step
+    auto set_weights = [&](int n) {
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int j = 32 * s + 8 * g + k;
+                weight[s][k] = j < n ? W.by_new * decay_power(log_decay, (float)(n - 1 - j + (W.from_end ? 1 : 0))) : 0.0f;
+            }
     };
-    auto write_weights = [&](int n) {
-        if ((int)threadIdx.x < C)
-            weight[threadIdx.x] = (int)threadIdx.x < n ? W.by_new * decay_power(log_decay, (float)(n - 1 - (int)threadIdx.x + (W.from_end ? 1 : 0))) : 0.0f;
-    };
-    if (length > 0) fetch(length, sy);
-    write_weights((int)(length < C ? length : C));
-    int half = 0;                                  // the tile of Y in use
-    for (long long at = 0; at < length; at += C, half ^= kDirectly) {
-        const int n = (int)(length - at < C ? length - at : C);
-        bf16_t *const y_now = sy + half * C * AP;
+    if (length > 0) {
+        if (reads) next_x.load(sx, tokens(length));
+        next_y.load(sy, tokens(length));
+        next_z.load(sz, tokens(length));
+    }
+    set_weights(tokens(length));
+    const Decay whole_block(log_decay, (float)C);
+    long long at = 0;
+    auto take_block = [&](bf16_t *const y_now, bf16_t *const y_next) __attribute__((always_inline)) {
+        const int n = tokens(length - at);
+        const long long left = length - at - C;                // behind this block
         const int row_at = here(row_lane<AP>(lane)), p_at = here(row_lane<C>(lane)), y_at = here(column_lane<AP, 8>(lane, 0)), z_at = here(column_lane<EB, 4 * CT>(lane, wave_e));
         if constexpr (kDirectly) {
             __builtin_amdgcn_s_waitcnt(kLoadsDone);
@@ -448,7 +455,7 @@ template <int DT, int AP, int CT, bool WHOLE> __global__ __launch_bounds__(64 * 
             next_z.store(sz, n);
         }
         __syncthreads();
-        if (n < C && at > 0) write_weights(n);     // (everybody has done with the block before, and reads them behind the next barrier)
+        if (n < C && at > 0) set_weights(n);
         if (reads) {
             // P^T, 16 keys by 16 queries at a time: the wavefronts take every fourth of the tiles on and below the diagonal, each all of its own at once
             constexpr int kPTiles = kTiles * (kTiles + 1) / 2, kMine = (kPTiles + kWalkWaves - 1) / kWalkWaves;
@@ -526,8 +533,8 @@ template <int DT, int AP, int CT, bool WHOLE> __global__ __launch_bounds__(64 * 
         }
         __builtin_amdgcn_sched_barrier(0);
         __syncthreads();                           // (X and Z have been read)
-        if (at + C < length) fetch(length - at - C, sy + (half ^ kDirectly) * C * AP);
         if (reads) {
+            if (left > 0) next_x.load(sx, tokens(left));
 #pragma unroll
             for (int t = 0; t < kTiles; ++t)
 #pragma unroll
@@ -555,8 +562,9 @@ template <int DT, int AP, int CT, bool WHOLE> __global__ __launch_bounds__(64 * 
             }
             out += C * out_step;
         }
+        if (left > 0) next_z.load(sz, tokens(left));
         // the state
-        const Decay decay(log_decay, (float)n);
+        const Decay decay = n == C ? whole_block : Decay(log_decay, (float)n);
         if (decay.slow)
 #pragma unroll
             for (int t = 0; t < AP / 16; ++t)
@@ -570,14 +578,14 @@ template <int DT, int AP, int CT, bool WHOLE> __global__ __launch_bounds__(64 * 
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
             __builtin_amdgcn_sched_barrier(0);
-            const f32x8 w = *(const f32x8 *)(weight + 32 * s + 8 * g);
+            if (s == kSteps - 1 && left > 0) next_y.load(y_next, tokens(left));
             Parts<3> wz[CT];
 #pragma unroll
             for (int c = 0; c < CT; ++c) {
                 f32x8 v = __builtin_convertvector(zt[s][c].p[N - 1], f32x8);
 #pragma unroll
                 for (int m = N - 2; m >= 0; --m) v += __builtin_convertvector(zt[s][c].p[m], f32x8);
-                wz[c] = split<3>(v * w);
+                wz[c] = split<3>(v * weight[s]);
             }
 #pragma unroll
             for (int t = 0; t < AP / 16; t += 2) {
@@ -598,6 +606,11 @@ template <int DT, int AP, int CT, bool WHOLE> __global__ __launch_bounds__(64 * 
                 products<2>(add, yt[0], Parts<2>());
             }
         }
+        at += C;
+    };
+    while (at < length) {
+        take_block(sy, kDirectly ? sy_too : sy);
+        if (kDirectly && at < length) take_block(sy_too, sy);
     }
     const size_t m_a = reads ? W.m_a : W.E, m_e = reads ? W.m_e : 1;
     each_of_state<AP, CT>(M, to != nullptr, e0 + wave_e, W.A, W.E, m_a, m_e, [&](float &m, size_t i) { to[i] = m; });
