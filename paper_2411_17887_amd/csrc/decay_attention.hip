@@ -41,12 +41,13 @@ struct WalkArgs {
     const long long *offsets, *slots;              // slots: null, or the state that each row has
     const float *m_in;                             // null: zeros
     float *m_out;                                  // null: not wanted
-    float *between;                                // [piece][head][A][E]: what segments add, then what they start from
+    float *between;                                // [piece][head][state]: what segments add, then what they start from
     void *ws;
     long long states;                              // how many states there are
     long long total;
     unsigned rows, heads, A, E;
     unsigned m_a, m_e;                             // strides of a state: M[a][e] is at a * m_a + e * m_e
+    unsigned between_a, between_e;                 // and of those between segments
     unsigned pieces, segment_log2;
     float by_new, by_read;
     int from_end;
@@ -359,14 +360,16 @@ template <int AP, int CT, class What> __device__ __forceinline__ void each_of_st
             }
 }
 
-template <int DT, int AP, int CT, bool WHOLE> __global__ __launch_bounds__(64 * kWalkWaves, groups_at_once(DT, AP, CT)) void walk_kernel(WalkArgs W)
+// READS: writes outputs and, of a row's last segment, the state.  Otherwise only what each segment but the last adds to the state.
+template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bounds__(64 * kWalkWaves, groups_at_once(DT, AP, CT)) void walk_kernel(WalkArgs W)
 {
     typedef typename Elem<DT>::T T;
     constexpr int N = parts_of(DT), C = block_tokens(DT, AP), EB = 16 * kWalkWaves * CT, kThreads = 64 * kWalkWaves;
     constexpr bool kDirectly = way_of(DT, WHOLE) == kDirect;
     constexpr int kTiles = C / 16, kSteps = C / 32, kOrder = N == 3 ? 3 : 2;       // tiles of 16 tokens, steps of 32
-    __shared__ __attribute__((aligned(16))) bf16_t sx[N * C * AP], sy[N * C * AP], sz[N * C * EB], sp[N * C * C];
-    __shared__ __attribute__((aligned(16))) bf16_t sy_too[kDirectly ? C * AP : 8];           // (an array of its own: loads into the one are not waited for to read the other)
+    __shared__ __attribute__((aligned(16))) bf16_t sy[N * C * AP], sz[N * C * EB], sx[READS ? N * C * AP : 8], sp[READS ? N * C * C : 8];
+    // (arrays of their own: loads into the one are not waited for to read the other)
+    __shared__ __attribute__((aligned(16))) bf16_t sy_too[kDirectly ? C * AP : 8], sz_too[kDirectly && !READS ? C * EB : 8];
 
     const unsigned blocks = (W.E + EB - 1) / EB;
     const unsigned block = blockIdx.x % blocks, h = blockIdx.x / blocks % W.heads, number = blockIdx.x / blocks / W.heads;
@@ -379,8 +382,7 @@ template <int DT, int AP, int CT, bool WHOLE> __global__ __launch_bounds__(64 * 
         }
     Piece piece;
     if (!find_piece(W, number, piece)) return;
-    const bool reads = W.out.data != nullptr;
-    if (!reads && piece.last) return;              // (what a row's last segment adds, nobody asks for)
+    if (!READS && piece.last) return;              // (what a row's last segment adds, nobody asks for)
 
     const float log_decay = W.log_decay[h];
     const int e0 = (int)block * EB, wave_e = 16 * CT * wave;        // the workgroup's first column, and the wavefront's of these
@@ -392,14 +394,14 @@ template <int DT, int AP, int CT, bool WHOLE> __global__ __launch_bounds__(64 * 
     f32x4 M[AP / 16][CT] = {};
     {
         // a row of several segments finds what it starts from in the workspace, also for the first of them
-        const float *from = !reads ? nullptr : cut ? W.between + between : W.m_in && slot >= 0 ? W.m_in + state : nullptr;
-        const size_t m_a = cut ? W.E : W.m_a, m_e = cut ? 1 : W.m_e;
+        const float *from = !READS ? nullptr : cut ? W.between + between : W.m_in && slot >= 0 ? W.m_in + state : nullptr;
+        const size_t m_a = cut ? W.between_a : W.m_a, m_e = cut ? W.between_e : W.m_e;
         each_of_state<AP, CT>(M, from != nullptr, e0 + wave_e, W.A, W.E, m_a, m_e, [&](float &m, size_t i) { m = from[i]; });
     }
     float reading[kTiles];                         // a^(i+1), from the end a^i, of the lane's token in each tile
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) reading[t] = decay_power(log_decay, (float)(16 * t + l + (W.from_end ? 0 : 1)));
-    if (reads)                                     // P above its diagonal of tiles: zeros for good
+    if (READS)                                     // P above its diagonal of tiles: zeros for good
         for (int i = threadIdx.x; i < N * (C / 32) * 16 * 2; i += kThreads) {
             const int n = i / (C / 32 * 32), t = i / 32 % (C / 32), row = i / 2 % 16, half = i % 2;
             *(u32x4 *)(sp + n * C * C + Tile<C>::at(32 * t + row, 32 * t + 16 + 8 * half)) = u32x4{0u, 0u, 0u, 0u};
@@ -417,12 +419,12 @@ template <int DT, int AP, int CT, bool WHOLE> __global__ __launch_bounds__(64 * 
     char *out = (char *)W.out.data + (W.out.at(h, W.heads) + origin * W.out.token) * out_size + (sign < 0 ? 15 * out_step : 0);
     typedef std::conditional_t<WHOLE, unsigned, long long> Offset;
     const Offset out_lane = (Offset)((sign < 0 ? l - 15 : l) * out_step) + (Offset)(col * out_size);         // (not negative: outputs have positive strides)
-    float *to = !reads ? W.between + between : piece.last && W.m_out && slot >= 0 ? W.m_out + state : nullptr;
+    float *to = !READS ? W.between + between : piece.last && W.m_out && slot >= 0 ? W.m_out + state : nullptr;
     // the third part of what is added to a state counts where the state itself is asked for, not where 16-bit outputs are read from it
     const bool exact = to || DT == kF32;
     const long long length = piece.end - piece.first;
-    // Loads of the next block start where their tiles in LDS have been read (Y has two) and a part of the work at a time: more of them at once than
-    // the memory pipeline takes hold up the wavefront.
+    // Loads of the next block start as soon as their tiles in LDS are free, a part of the work apart: more of them at once than the memory
+    // pipeline takes hold up the wavefront.
     auto tokens = [&](long long left) { return (int)(left < C ? left : C); };
     f32x8 weight[kSteps];                          // by_new a^(n-1-j), from the end a^(n-j), of the lane's tokens j of each step
     auto set_weights = [&](int n) {
@@ -435,14 +437,15 @@ template <int DT, int AP, int CT, bool WHOLE> __global__ __launch_bounds__(64 * 
             }
     };
     if (length > 0) {
-        if (reads) next_x.load(sx, tokens(length));
+        if constexpr (READS) next_x.load(sx, tokens(length));
         next_y.load(sy, tokens(length));
         next_z.load(sz, tokens(length));
     }
     set_weights(tokens(length));
     const Decay whole_block(log_decay, (float)C);
     long long at = 0;
-    auto take_block = [&](bf16_t *const y_now, bf16_t *const y_next) __attribute__((always_inline)) {
+    // (Y has two tiles in LDS if loads write there themselves, Z only where there are no outputs)
+    auto take_block = [&](bf16_t *const y_now, bf16_t *const y_next, bf16_t *const z_now, bf16_t *const z_next) __attribute__((always_inline)) {
         const int n = tokens(length - at);
         const long long left = length - at - C;                // behind this block
         const int row_at = here(row_lane<AP>(lane)), p_at = here(row_lane<C>(lane)), y_at = here(column_lane<AP, 8>(lane, 0)), z_at = here(column_lane<EB, 4 * CT>(lane, wave_e));
@@ -450,13 +453,17 @@ template <int DT, int AP, int CT, bool WHOLE> __global__ __launch_bounds__(64 * 
             __builtin_amdgcn_s_waitcnt(kLoadsDone);
         } else {
             __syncthreads();                       // everybody has done with the block before
-            if (reads) next_x.store(sx, n);
+            if constexpr (READS) next_x.store(sx, n);
             next_y.store(sy, n);
             next_z.store(sz, n);
         }
         __syncthreads();
+        if (kDirectly && left > 0) {
+            next_y.load(y_next, tokens(left));
+            if constexpr (!READS) next_z.load(z_next, tokens(left));
+        }
         if (n < C && at > 0) set_weights(n);
-        if (reads) {
+        if constexpr (READS) {
             // P^T, 16 keys by 16 queries at a time: the wavefronts take every fourth of the tiles on and below the diagonal, each all of its own at once
             constexpr int kPTiles = kTiles * (kTiles + 1) / 2, kMine = (kPTiles + kWalkWaves - 1) / kWalkWaves;
             int it[kMine], jt[kMine];
@@ -500,10 +507,10 @@ template <int DT, int AP, int CT, bool WHOLE> __global__ __launch_bounds__(64 * 
 #pragma unroll
             for (int c = 0; c < CT; ++c)
 #pragma unroll
-                for (int m = 0; m < N; ++m) zt[s][c].p[m] = column_operand<EB>(sz + m * C * EB, z_at, 32 * s, 4 * c);
+                for (int m = 0; m < N; ++m) zt[s][c].p[m] = column_operand<EB>(z_now + m * C * EB, z_at, 32 * s, 4 * c);
         constexpr int NM = N == 3 ? 3 : 2;
         f32x4 o[kTiles][CT];
-        if (reads) {
+        if constexpr (READS) {
 #pragma unroll
             for (int t = 0; t < kTiles; ++t)
 #pragma unroll
@@ -532,8 +539,8 @@ template <int DT, int AP, int CT, bool WHOLE> __global__ __launch_bounds__(64 * 
             }
         }
         __builtin_amdgcn_sched_barrier(0);
-        __syncthreads();                           // (X and Z have been read)
-        if (reads) {
+        if constexpr (READS) {
+            if constexpr (kDirectly) __syncthreads();          // (X and Z have been read)
             if (left > 0) next_x.load(sx, tokens(left));
 #pragma unroll
             for (int t = 0; t < kTiles; ++t)
@@ -562,7 +569,8 @@ template <int DT, int AP, int CT, bool WHOLE> __global__ __launch_bounds__(64 * 
             }
             out += C * out_step;
         }
-        if (left > 0) next_z.load(sz, tokens(left));
+        if ((READS || !kDirectly) && left > 0) next_z.load(sz, tokens(left));
+        if (!kDirectly && left > 0) next_y.load(sy, tokens(left));
         // the state
         const Decay decay = n == C ? whole_block : Decay(log_decay, (float)n);
         if (decay.slow)
@@ -578,7 +586,6 @@ template <int DT, int AP, int CT, bool WHOLE> __global__ __launch_bounds__(64 * 
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
             __builtin_amdgcn_sched_barrier(0);
-            if (s == kSteps - 1 && left > 0) next_y.load(y_next, tokens(left));
             Parts<3> wz[CT];
 #pragma unroll
             for (int c = 0; c < CT; ++c) {
@@ -609,15 +616,15 @@ template <int DT, int AP, int CT, bool WHOLE> __global__ __launch_bounds__(64 * 
         at += C;
     };
     while (at < length) {
-        take_block(sy, kDirectly ? sy_too : sy);
-        if (kDirectly && at < length) take_block(sy_too, sy);
+        take_block(sy, sy_too, sz, sz_too);
+        if (kDirectly && at < length) take_block(sy_too, sy, READS ? sz : sz_too, sz);
     }
-    const size_t m_a = reads ? W.m_a : W.E, m_e = reads ? W.m_e : 1;
+    const size_t m_a = READS ? W.m_a : W.between_a, m_e = READS ? W.m_e : W.between_e;
     each_of_state<AP, CT>(M, to != nullptr, e0 + wave_e, W.A, W.E, m_a, m_e, [&](float &m, size_t i) { to[i] = m; });
 }
 
 // What each segment of a row starts from, from what the segments in front of it add: a thread takes one element of the state along the row.
-constexpr int kJoinThreads = 256;
+constexpr int kJoinThreads = 256, kJoinAhead = 8;
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(WalkArgs W)
 {
     const unsigned size = W.A * W.E, blocks = (size + kJoinThreads - 1) / kJoinThreads;
@@ -628,17 +635,21 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(WalkArgs W)
     const long long segment = 1ll << W.segment_log2, segments = (hi - lo + segment - 1) >> W.segment_log2, first = (lo >> W.segment_log2) + r;
     if (segments <= 1 || first + segments > (long long)W.pieces) return;
     const long long slot = state_of(W.slots, r, W.states);
-    const unsigned a = i / W.E, e = i % W.E;
+    const unsigned a = W.between_e == 1 ? i / W.E : i % W.A, e = W.between_e == 1 ? i % W.E : i / W.A;         // element i of a state between segments
     float m = W.m_in && slot >= 0 ? W.m_in[((size_t)slot * W.heads + h) * size + (size_t)a * W.m_a + (size_t)e * W.m_e] : 0.0f;
     const Decay decay(W.log_decay[h], (float)segment);
     float *p = W.between + ((size_t)first * W.heads + h) * size + i;
     const size_t step = (size_t)W.heads * size;
-    for (long long s = 0; s + 1 < segments; ++s, p += step) {
-        const float added = *p;
-        *p = m;
-        m = decay(m) + added;
+    for (long long s = 0; s < segments; s += kJoinAhead) {
+        float added[kJoinAhead];                   // (of the last segment nothing is known, nor asked for)
+#pragma unroll
+        for (int u = 0; u < kJoinAhead; ++u) added[u] = s + u + 1 < segments ? p[(s + u) * step] : 0.0f;
+#pragma unroll
+        for (int u = 0; u < kJoinAhead; ++u) {
+            if (s + u < segments) p[(s + u) * step] = m;
+            m = decay(m) + added[u];
+        }
     }
-    *p = m;
 }
 
 // out[t][stored head][i] = the sum of part[t][head][i] over the heads that share the stored head.
@@ -768,11 +779,14 @@ tcuscan_status_t check_shape(const tcuscan_attention_shape_t *p, int dt)
     return TCUSCAN_OK;
 }
 
-// Rows are cut into segments so that a call with few rows and heads still has a workgroup or two for every compute unit.
+// Rows are cut into segments so that a call with few rows and heads still has a workgroup or two for every compute unit, but not below 128 tokens; calls
+// of up to 512 tokens are not cut (three launches then take longer than eight blocks in a row).
 constexpr size_t kWantedGroups = 512;
-constexpr unsigned kMinSegmentLog2 = 9, kWholeRows = 62;
+constexpr unsigned kMinSegmentLog2 = 7, kWholeRows = 62;
+constexpr long long kMostUncut = 512;
 unsigned segment_log2_for(const tcuscan_attention_shape_t &s)
 {
+    if (s.total <= kMostUncut) return kWholeRows;
     const size_t blocks = (size_t)((s.dk > s.dv ? s.dk : s.dv) + 127) / 128;
     unsigned log2 = kMinSegmentLog2;
     while (((size_t)s.total * s.heads * blocks) >> log2 > kWantedGroups) ++log2;
@@ -802,14 +816,16 @@ bool misaligned(const void *p, size_t to) { return (uintptr_t)p % to != 0; }
 
 Heads heads_of(const void *data, long long token, long long head, long long heads) { return {(void *)data, token, head, (unsigned)heads}; }
 
-template <int DT, int CT, bool WHOLE> const void *walk_for(unsigned A)
+template <int DT, int CT, bool WHOLE, bool READS> const void *walk_for(unsigned A)
 {
-    return A <= 32 ? (const void *)walk_kernel<DT, 32, CT, WHOLE> : A <= 64 ? (const void *)walk_kernel<DT, 64, CT, WHOLE>
-         : A <= 128 ? (const void *)walk_kernel<DT, 128, CT, WHOLE> : (const void *)walk_kernel<DT, 256, 1, WHOLE>;
+    return A <= 32 ? (const void *)walk_kernel<DT, 32, CT, WHOLE, READS> : A <= 64 ? (const void *)walk_kernel<DT, 64, CT, WHOLE, READS>
+         : A <= 128 ? (const void *)walk_kernel<DT, 128, CT, WHOLE, READS> : (const void *)walk_kernel<DT, 256, 1, WHOLE, READS>;
 }
-template <int CT, bool WHOLE> const void *walk_for(int dt, unsigned A)
+template <int DT, int CT, bool READS> const void *walk_for(unsigned A, bool whole) { return whole ? walk_for<DT, CT, true, READS>(A) : walk_for<DT, CT, false, READS>(A); }
+template <int DT, bool READS> const void *walk_for(unsigned A, bool whole, unsigned tiles) { return tiles == 1 ? walk_for<DT, 1, READS>(A, whole) : walk_for<DT, 2, READS>(A, whole); }
+template <bool READS> const void *walk_for(int dt, unsigned A, bool whole, unsigned tiles)
 {
-    return dt == kF16 ? walk_for<kF16, CT, WHOLE>(A) : dt == kF32 ? walk_for<kF32, CT, WHOLE>(A) : walk_for<kBF16, CT, WHOLE>(A);
+    return dt == kF16 ? walk_for<kF16, READS>(A, whole, tiles) : dt == kF32 ? walk_for<kF32, READS>(A, whole, tiles) : walk_for<kBF16, READS>(A, whole, tiles);
 }
 
 // Whether groups of eight elements of every token's features are aligned and whole, and 64 tokens within reach of a 32-bit offset.
@@ -819,8 +835,9 @@ bool whole(const Heads &x, unsigned dims, size_t esz)
            (x.token < 0 ? -x.token : x.token) < (1ll << 22);
 }
 
-// One walk, into `out`; with heads that share the output, into `part` first.
-tcuscan_status_t walk(WalkArgs W, Heads out, float *part, int dt, hipStream_t s)
+// One walk, into `out`; with heads that share the output, into `part` first.  `states_ready`: a walk with the same states, or transposed ones, has
+// left what the segments start from in the workspace.
+tcuscan_status_t walk(WalkArgs W, Heads out, float *part, int dt, hipStream_t s, bool states_ready = false)
 {
     const size_t esz = elem_bytes(dt);
     const unsigned tiles = W.E <= 64 || W.A > 128 ? 1 : 2, cols = 64 * tiles;           // (256 rows of a state and 32 columns do not fit the registers)
@@ -830,16 +847,13 @@ tcuscan_status_t walk(WalkArgs W, Heads out, float *part, int dt, hipStream_t s)
     const bool shared = out.heads < W.heads;
     const Heads to = shared ? Heads{part, (long long)W.heads * W.E, W.E, W.heads} : out;
     W.wide = shared;
-    const bool all_whole = whole(W.x, W.A, esz) && whole(W.y, W.A, esz) && whole(W.z, W.E, esz) && whole(to, W.E, shared ? 4 : esz) && to.token > 0;
-    const void *fn = tiles == 1 ? all_whole ? walk_for<1, true>(dt, W.A) : walk_for<1, false>(dt, W.A)
-                                : all_whole ? walk_for<2, true>(dt, W.A) : walk_for<2, false>(dt, W.A);
-    if (W.segment_log2 != kWholeRows) {
-        W.out = Heads{};
-        if (!launch(fn, groups, 64 * kWalkWaves, &W, s) || !launch((const void *)join_kernel, join_groups, kJoinThreads, &W, s)) return TCUSCAN_ERR_HIP;
+    const bool new_whole = whole(W.y, W.A, esz) && whole(W.z, W.E, esz), all_whole = new_whole && whole(W.x, W.A, esz) && whole(to, W.E, shared ? 4 : esz) && to.token > 0;
+    if (W.segment_log2 != kWholeRows && !states_ready) {
+        if (!launch(walk_for<false>(dt, W.A, new_whole, tiles), groups, 64 * kWalkWaves, &W, s) || !launch((const void *)join_kernel, join_groups, kJoinThreads, &W, s))
+            return TCUSCAN_ERR_HIP;
     }
     W.out = to;
-    if (!W.out.data) W.out.data = W.ws;            // (no tokens: nothing is written there)
-    if (!launch(fn, groups, 64 * kWalkWaves, &W, s)) return TCUSCAN_ERR_HIP;
+    if (!launch(walk_for<true>(dt, W.A, all_whole, tiles), groups, 64 * kWalkWaves, &W, s)) return TCUSCAN_ERR_HIP;
     const size_t items = (size_t)W.total * out.heads * W.E;
     if (!shared || !items) return TCUSCAN_OK;
     SumArgs S = {part, out, W.total, W.heads, W.E};
@@ -881,7 +895,7 @@ tcuscan_status_t tcuscan_decay_attention(const tcuscan_attention_shape_t *shape,
     W.log_decay = d_log_decay; W.offsets = d_offsets; W.slots = d_slots; W.m_in = d_state_in; W.m_out = d_state_out; W.ws = d_ws;
     W.between = (float *)((char *)d_ws + L.between); W.segment_log2 = L.segment_log2; W.pieces = (unsigned)pieces_for(p, L.segment_log2);
     W.states = (long long)states; W.total = p.total; W.rows = (unsigned)p.rows; W.heads = (unsigned)p.heads;
-    W.A = (unsigned)p.dk; W.E = (unsigned)p.dv; W.m_a = W.E; W.m_e = 1;
+    W.A = (unsigned)p.dk; W.E = (unsigned)p.dv; W.m_a = W.between_a = W.E; W.m_e = W.between_e = 1;
     W.by_new = 1.0f; W.by_read = scale; W.from_end = 0;
     return walk(W, heads_of(d_out, p.o_token, p.o_head, p.heads), nullptr, dt, (hipStream_t)stream);
 }
@@ -921,18 +935,21 @@ tcuscan_status_t tcuscan_decay_attention_backward(const tcuscan_attention_shape_
     W.between = (float *)((char *)d_ws + L.between); W.segment_log2 = L.segment_log2; W.pieces = (unsigned)pieces_for(p, L.segment_log2);
     W.states = p.rows; W.total = p.total; W.rows = (unsigned)p.rows; W.heads = (unsigned)p.heads;
     const unsigned dk = (unsigned)p.dk, dv = (unsigned)p.dv;
-    // dq, with the states of the forward pass
+    // dq, with the states of the forward pass: S^T
     W.x = o; W.y = v; W.z = k; W.A = dv; W.E = dk; W.m_a = 1; W.m_e = dv; W.m_in = d_state_in;
+    W.between_a = dk; W.between_e = 1;
     W.by_new = 1.0f; W.by_read = scale; W.from_end = 0;
     tcuscan_status_t r = walk(W, heads_of(d_q_grad, p.dq_token, p.dq_head, p.q_heads), part, dt, s);
     if (r != TCUSCAN_OK) return r;
-    // dk, dv and the gradient by the first states, from the end
-    W.by_new = scale; W.by_read = 1.0f; W.from_end = 1; W.m_in = d_state_out_grad;
-    W.x = v; W.y = o; W.z = q;
-    r = walk(W, heads_of(d_k_grad, p.dk_token, p.dk_head, p.k_heads), part, dt, s);
+    // dv and the gradient by the first states, from the end: R
+    W.by_new = scale; W.by_read = 1.0f; W.from_end = 1; W.m_in = d_state_out_grad; W.m_out = d_state_in_grad;
+    W.x = k; W.y = q; W.z = o; W.A = dk; W.E = dv; W.m_a = W.between_a = dv; W.m_e = W.between_e = 1;
+    r = walk(W, heads_of(d_v_grad, p.dv_token, p.dv_head, p.v_heads), part, dt, s);
     if (r != TCUSCAN_OK) return r;
-    W.x = k; W.y = q; W.z = o; W.A = dk; W.E = dv; W.m_a = dv; W.m_e = 1; W.m_out = d_state_in_grad;
-    return walk(W, heads_of(d_v_grad, p.dv_token, p.dv_head, p.v_heads), part, dt, s);
+    // dk, with the same states, transposed: R^T.  What its segments start from is there.
+    W.m_out = nullptr;
+    W.x = v; W.y = o; W.z = q; W.A = dv; W.E = dk; W.m_a = W.between_a = 1; W.m_e = W.between_e = dv;
+    return walk(W, heads_of(d_k_grad, p.dk_token, p.dk_head, p.k_heads), part, dt, s, true);
 }
 
 tcuscan_status_t tcuscan_decay_attention_step(const tcuscan_attention_shape_t *shape, const void *d_q, const void *d_k, const void *d_v, void *d_out,
