@@ -70,6 +70,26 @@ struct Decay {
     __device__ __forceinline__ float operator()(float m) const { return fmaf(m, by, slow ? m : 0.0f); }
 };
 
+// The same for many steps of n tokens each, one multiplication per element: what rounding takes from a^n, by() adds to a later factor, so that the
+// product of all factors stays within an ulp or two of the decay.
+struct Decays {
+    float factor, less, owed;                      // a^n = factor + less
+    __device__ __forceinline__ Decays(float log_decay, float n)
+    {
+        const Decay d(log_decay, n);
+        factor = d.slow ? 1.0f + d.by : d.by;
+        less = d.slow ? d.by - (factor - 1.0f) : 0.0f;
+        owed = 0.0f;
+    }
+    __device__ __forceinline__ float by()
+    {
+        owed += less;
+        const float f = factor + owed;
+        owed -= f - factor;
+        return f;
+    }
+};
+
 // Row r's tokens, clipped to the arrays.
 __device__ __forceinline__ void row_extent(const long long *offsets, unsigned r, long long total, long long &lo, long long &hi)
 {
@@ -323,12 +343,12 @@ __device__ __forceinline__ bool find_piece(const WalkArgs &W, unsigned number, P
 }
 
 // K consecutive columns of the output, `col` the first of them.  WHOLE: they are aligned and all inside or all outside.
-template <class T, bool WHOLE, int K> __device__ __forceinline__ void store_columns(T *p, int col, int cols, const f32x4 *v, float by)
+template <class T, bool WHOLE, int K> __device__ __forceinline__ void store_columns(T *p, int col, int cols, const f32x4 *v)
 {
     typedef T Some __attribute__((ext_vector_type(K)));
     Some x;
 #pragma unroll
-    for (int k = 0; k < K; ++k) x[k] = (T)(v[k / 4][k % 4] * by);
+    for (int k = 0; k < K; ++k) x[k] = (T)v[k / 4][k % 4];
     if constexpr (WHOLE) {
         if (col < cols) *(Some *)p = x;
     } else {
@@ -398,9 +418,10 @@ template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bo
         const size_t m_a = cut ? W.between_a : W.m_a, m_e = cut ? W.between_e : W.m_e;
         each_of_state<AP, CT>(M, from != nullptr, e0 + wave_e, W.A, W.E, m_a, m_e, [&](float &m, size_t i) { m = from[i]; });
     }
-    float reading[kTiles];                         // a^(i+1), from the end a^i, of the lane's token in each tile
+    float reading[kTiles];                         // by_read a^(i+1), from the end a^i, of the lane's token in each tile
+    const float by_key = W.by_read * W.by_new;
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) reading[t] = decay_power(log_decay, (float)(16 * t + l + (W.from_end ? 0 : 1)));
+    for (int t = 0; t < kTiles; ++t) reading[t] = W.by_read * decay_power(log_decay, (float)(16 * t + l + (W.from_end ? 0 : 1)));
     if (READS)                                     // P above its diagonal of tiles: zeros for good
         for (int i = threadIdx.x; i < N * (C / 32) * 16 * 2; i += kThreads) {
             const int n = i / (C / 32 * 32), t = i / 32 % (C / 32), row = i / 2 % 16, half = i % 2;
@@ -421,7 +442,8 @@ template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bo
     const Offset out_lane = (Offset)((sign < 0 ? l - 15 : l) * out_step) + (Offset)(col * out_size);         // (not negative: outputs have positive strides)
     float *to = !READS ? W.between + between : piece.last && W.m_out && slot >= 0 ? W.m_out + state : nullptr;
     // the third part of what is added to a state counts where the state itself is asked for, not where 16-bit outputs are read from it
-    const bool exact = to || DT == kF32;
+    constexpr int kParts = !READS || N == 3 ? 3 : 2;
+    const bool exact = to != nullptr;
     const long long length = piece.end - piece.first;
     // Loads of the next block start as soon as their tiles in LDS are free, a part of the work apart: more of them at once than the memory
     // pipeline takes hold up the wavefront.
@@ -442,7 +464,7 @@ template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bo
         next_z.load(sz, tokens(length));
     }
     set_weights(tokens(length));
-    const Decay whole_block(log_decay, (float)C);
+    Decays whole_block(log_decay, (float)C);
     long long at = 0;
     // (Y has two tiles in LDS if loads write there themselves, Z only where there are no outputs)
     auto take_block = [&](bf16_t *const y_now, bf16_t *const y_next, bf16_t *const z_now, bf16_t *const z_next) __attribute__((always_inline)) {
@@ -464,38 +486,54 @@ template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bo
         }
         if (n < C && at > 0) set_weights(n);
         if constexpr (READS) {
-            // P^T, 16 keys by 16 queries at a time: the wavefronts take every fourth of the tiles on and below the diagonal, each all of its own at once
-            constexpr int kPTiles = kTiles * (kTiles + 1) / 2, kMine = (kPTiles + kWalkWaves - 1) / kWalkWaves;
+            // P^T, 16 keys by 16 queries at a time.  Of the ten tiles on and below the diagonal each wavefront takes two or three that share operands:
+            // queries' tile 3 with keys' 0 and 1 | 3 with 2 and 3 | 2 with 0, 1 and 2 | 1 with 0 and 1, 0 with 0; of three: 0 with 0 | 1 with 0 | 1 with 1 | none
+            constexpr int kMine = kTiles == 4 ? 3 : 1;
+            const int mine = kTiles == 4 ? wave < 2 ? 2 : 3 : wave < 3 ? 1 : 0;
             int it[kMine], jt[kMine];
-            f32x4 p[kMine];
 #pragma unroll
             for (int k = 0; k < kMine; ++k) {
-                const int tile = min(wave + k * kWalkWaves, kPTiles - 1);
-                it[k] = tile >= 6 ? 3 : tile >= 3 ? 2 : tile >= 1 ? 1 : 0;
-                jt[k] = tile - it[k] * (it[k] + 1) / 2;
-                p[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                it[k] = kTiles == 4 ? wave < 2 ? 3 : wave == 2 ? 2 : k < 2 ? 1 : 0 : wave > 0 ? 1 : 0;
+                jt[k] = kTiles == 4 ? wave == 1 ? 2 + (k & 1) : wave == 3 ? k & 1 : k : wave == 2 ? 1 : 0;
             }
+            f32x4 p[kMine];
 #pragma unroll
-            for (int s = 0; s < AP / 32; ++s)
+            for (int k = 0; k < kMine; ++k) p[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int k = 0; k < kMine; ++k) {
-                    Parts<N> a, b;
+            for (int s = 0; s < AP / 32; ++s) {
+                Parts<N> keys[kMine], queries;
+#pragma unroll
+                for (int m = 0; m < N; ++m) {
+                    queries.p[m] = row_operand<AP>(sx + m * C * AP, row_at, 16 * it[0], 32 * s);
+#pragma unroll
+                    for (int k = 0; k < (kMine < 2 ? kMine : 2); ++k) keys[k].p[m] = row_operand<AP>(y_now + m * C * AP, row_at, 16 * jt[k], 32 * s);
+                }
+                products<kOrder>([&](int i, int j) {
+#pragma unroll
+                    for (int k = 0; k < (kMine < 2 ? kMine : 2); ++k) p[k] = mfma(keys[k].p[i], queries.p[j], p[k]);
+                }, keys[0], queries);
+            }
+            if (kMine > 2 && mine > 2)
+#pragma unroll
+                for (int s = 0; s < AP / 32; ++s) {
+                    Parts<N> keys, queries;
 #pragma unroll
                     for (int m = 0; m < N; ++m) {
-                        a.p[m] = row_operand<AP>(y_now + m * C * AP, row_at, 16 * jt[k], 32 * s);
-                        b.p[m] = row_operand<AP>(sx + m * C * AP, row_at, 16 * it[k], 32 * s);
+                        queries.p[m] = row_operand<AP>(sx + m * C * AP, row_at, 16 * it[kMine - 1], 32 * s);
+                        keys.p[m] = row_operand<AP>(y_now + m * C * AP, row_at, 16 * jt[kMine - 1], 32 * s);
                     }
-                    products<kOrder>([&](int i, int j) { p[k] = mfma(a.p[i], b.p[j], p[k]); }, a, b);
+                    products<kOrder>([&](int i, int j) { p[kMine - 1] = mfma(keys.p[i], queries.p[j], p[kMine - 1]); }, keys, queries);
                 }
 #pragma unroll
             for (int k = 0; k < kMine; ++k) {
+                if (k >= mine) break;
                 const int i = 16 * it[k] + l, j = 16 * jt[k] + 4 * g, apart = here(i - j);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) p[k][r] = apart >= r ? p[k][r] * (W.by_new * decay_power(log_decay, (float)(apart - r))) : 0.0f;
+                for (int r = 0; r < 4; ++r) p[k][r] = apart >= r ? p[k][r] * (by_key * decay_power(log_decay, (float)(apart - r))) : 0.0f;
 #pragma unroll
                 for (int m = 0; m < N; ++m) {
                     const bf16x4 part = __builtin_convertvector(p[k], bf16x4);
-                    if (wave + k * kWalkWaves < kPTiles) *(bf16x4 *)(sp + m * C * C + Tile<C>::at(i, j)) = part;
+                    *(bf16x4 *)(sp + m * C * C + Tile<C>::at(i, j)) = part;
                     p[k] -= __builtin_convertvector(part, f32x4);
                 }
             }
@@ -508,6 +546,36 @@ template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bo
             for (int c = 0; c < CT; ++c)
 #pragma unroll
                 for (int m = 0; m < N; ++m) zt[s][c].p[m] = column_operand<EB>(z_now + m * C * EB, z_at, 32 * s, 4 * c);
+        auto whole_z = [&](int s, int c) {
+            f32x8 v = __builtin_convertvector(zt[s][c].p[N - 1], f32x8);
+#pragma unroll
+            for (int m = N - 2; m >= 0; --m) v += __builtin_convertvector(zt[s][c].p[m], f32x8);
+            return v;
+        };
+        Parts<kParts> wz[2][CT];                   // what is added to the state, of this step of 32 tokens and of the next
+        auto weigh = [&](int s) {
+#pragma unroll
+            for (int c = 0; c < CT; ++c) wz[s & 1][c] = split<kParts>(whole_z(s, c) * weight[s]);
+        };
+        // the state decays and the first step is weighted next to other products
+        auto begin_update = [&] {
+            weigh(0);
+            const float by = n == C ? whole_block.by() : Decays(log_decay, (float)n).by();
+#pragma unroll
+            for (int t = 0; t < AP / 16; ++t)
+#pragma unroll
+                for (int c = 0; c < CT; ++c) M[t][c] *= by;
+            if constexpr (READS) {                 // (here, where products run that need nothing of it, and not where it is used)
+#pragma unroll
+                for (int c = 0; c < CT; ++c)
+#pragma unroll
+                    for (int i = 0; i < kParts; ++i) asm volatile("" : "+v"(wz[0][c].p[i]));
+#pragma unroll
+                for (int t = 0; t < AP / 16; ++t)
+#pragma unroll
+                    for (int c = 0; c < CT; ++c) asm volatile("" : "+v"(M[t][c]));
+            }
+        };
         constexpr int NM = N == 3 ? 3 : 2;
         f32x4 o[kTiles][CT];
         if constexpr (READS) {
@@ -530,6 +598,7 @@ template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bo
 #pragma unroll
                     for (int i = 0; i < N; ++i) b[t].p[i] = row_operand<AP>(sx + i * C * AP, row_at, 16 * t, 32 * s);
                 if (s + 1 < AP / 32) split_m(s + 1);
+                else begin_update();
                 products<kOrder>([&](int i, int j) {           // (independent ones behind each other)
 #pragma unroll
                     for (int c = 0; c < CT; ++c)
@@ -564,55 +633,53 @@ template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bo
             for (int t = 0; t < kTiles; ++t) {
                 if (16 * t + l >= n) continue;
                 char *to_row = out + 16 * t * out_step + out_lane;
-                if (W.wide) store_columns<float, WHOLE, 4 * CT>((float *)to_row, col, (int)W.E, o[t], W.by_read);
-                else store_columns<T, WHOLE, 4 * CT>((T *)to_row, col, (int)W.E, o[t], W.by_read);
+                if (W.wide) store_columns<float, WHOLE, 4 * CT>((float *)to_row, col, (int)W.E, o[t]);
+                else store_columns<T, WHOLE, 4 * CT>((T *)to_row, col, (int)W.E, o[t]);
             }
             out += C * out_step;
         }
+        if constexpr (!READS) begin_update();
         if ((READS || !kDirectly) && left > 0) next_z.load(sz, tokens(left));
         if (!kDirectly && left > 0) next_y.load(sy, tokens(left));
-        // the state
-        const Decay decay = n == C ? whole_block : Decay(log_decay, (float)n);
-        if (decay.slow)
-#pragma unroll
-            for (int t = 0; t < AP / 16; ++t)
-#pragma unroll
-                for (int c = 0; c < CT; ++c) M[t][c] = __builtin_elementwise_fma(M[t][c], f32x4{decay.by, decay.by, decay.by, decay.by}, M[t][c]);
-        else
-#pragma unroll
-            for (int t = 0; t < AP / 16; ++t)
-#pragma unroll
-                for (int c = 0; c < CT; ++c) M[t][c] *= decay.by;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
             __builtin_amdgcn_sched_barrier(0);
-            Parts<3> wz[CT];
-#pragma unroll
-            for (int c = 0; c < CT; ++c) {
-                f32x8 v = __builtin_convertvector(zt[s][c].p[N - 1], f32x8);
-#pragma unroll
-                for (int m = N - 2; m >= 0; --m) v += __builtin_convertvector(zt[s][c].p[m], f32x8);
-                wz[c] = split<3>(v * weight[s]);
-            }
-#pragma unroll
-            for (int t = 0; t < AP / 16; t += 2) {
-                Parts<N> yt[2];
+            Parts<N> yt[2][2];                     // two tiles of M's rows, and the next two
+            auto load_y = [&](int t) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
 #pragma unroll
-                    for (int m = 0; m < N; ++m) yt[u].p[m] = column_operand<AP>(y_now + m * C * AP, y_at, 32 * s, 16 * t + 4 * u);
-                auto add = [&](int i, int j) {
+                    for (int m = 0; m < N; ++m) yt[t / 2 & 1][u].p[m] = column_operand<AP>(y_now + m * C * AP, y_at, 32 * s, 16 * t + 4 * u);
+            };
+            load_y(0);
+#pragma unroll
+            for (int t = 0; t < AP / 16; t += 2) {
+                if (t + 2 < AP / 16) load_y(t + 2);
+                products<kParts>([&](int i, int j) {
 #pragma unroll
                     for (int u = 0; u < 2; ++u)
 #pragma unroll
-                        for (int c = 0; c < CT; ++c) M[t + u][c] = mfma(yt[u].p[i], wz[c].p[j], M[t + u][c]);
-                };
-                if (exact)
-#pragma unroll
-                    for (int i = 0; i < N; ++i) add(i, 2 - i);
-                products<2>(add, yt[0], Parts<2>());
+                        for (int c = 0; c < CT; ++c) M[t + u][c] = mfma(yt[t / 2 & 1][u].p[i], wz[s & 1][c].p[j], M[t + u][c]);
+                }, yt[0][0], wz[0][0]);
             }
+            if (s + 1 < kSteps) weigh(s + 1);
         }
+        if constexpr (kParts == 2)
+            if (exact)                             // the third parts
+#pragma unroll
+                for (int s = 0; s < kSteps; ++s) {
+                    Parts<3> third[CT];
+#pragma unroll
+                    for (int c = 0; c < CT; ++c) third[c] = split<3>(whole_z(s, c) * weight[s]);
+#pragma unroll
+                    for (int t = 0; t < AP / 16; ++t)
+#pragma unroll
+                        for (int m = 0; m < N; ++m) {
+                            const bf16x8 yt = column_operand<AP>(y_now + m * C * AP, y_at, 32 * s, 32 * (t / 2) + 4 * (t & 1));
+#pragma unroll
+                            for (int c = 0; c < CT; ++c) M[t][c] = mfma(yt, third[c].p[2 - m], M[t][c]);
+                        }
+                }
         at += C;
     };
     while (at < length) {
