@@ -22,6 +22,7 @@
 #include "../../include/tcuscan.h"
 #include "chain_layout.h"
 #include "element_types.h"
+#include "wave_ops.h"
 
 namespace {
 
@@ -41,13 +42,13 @@ struct WalkArgs {
     const long long *offsets, *slots;              // slots: null, or the state that each row has
     const float *m_in;                             // null: zeros
     float *m_out;                                  // null: not wanted
-    float *between;                                // [piece][head][state]: what segments add, then what they start from
+    float *between;                                // [piece][head][state]: what segments add, then what they start from, laid out as lanes hold it
+    float *between_turned;                         // null, or where what they start from goes transposed, too: for a walk with A and E exchanged
     void *ws;
     long long states;                              // how many states there are
     long long total;
     unsigned rows, heads, A, E;
     unsigned m_a, m_e;                             // strides of a state: M[a][e] is at a * m_a + e * m_e
-    unsigned between_a, between_e;                 // and of those between segments
     unsigned pieces, segment_log2;
     float by_new, by_read;
     int from_end;
@@ -120,8 +121,8 @@ __device__ __forceinline__ long long state_of(const long long *slots, unsigned r
 //
 // Precision.  The matrix unit multiplies bf16 and adds in fp32, so every operand is a sum of bf16 parts: bf16 inputs one, f16 two (exact),
 // fp32 three.  What is rounded on the way:
-//   * what is added to a state, by_new a^(C-1-j) z_j: three parts (24 bits), so that states come out as exact as fp32 sums make them; two (16 bits)
-//     where only 16-bit outputs are read from it
+//   * what is added to a state, by_new a^(C-1-j) z_j: three parts (24 bits) where the row's last state is asked for and this much of it is left there, so that
+//     states come out as exact as fp32 sums make them; two (16 bits) where only 16-bit outputs are read from it
 //   * the state, where it is read: two parts (16 bits), three for fp32
 //   * the weighted scores P: one part for bf16 (an error like the output's own rounding), two for f16, three for fp32
 // and products of parts that together lie below what is kept are left out (kOrder).
@@ -135,13 +136,15 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int parts_of(int dt) { return dt == kBF16 ? 1 : dt == kF16 ? 2 : 3; }
-// Tokens of a block: what LDS holds of X, Y and Z next to each other.
-constexpr int block_tokens(int dt, int ap) { return dt == kF32 || (dt == kF16 && ap > 128) ? 32 : 64; }
+// Tokens of a block.  With 64 the state would be read (split, multiplied) half as often, but LDS would hold no more than the next block beside the present
+// one: too little on its way to keep the memory busy (65536 tokens 400 us, of which the reading of inputs from L2 alone 300).
+constexpr int kBlock = 32;
 
 constexpr int kWalkWaves = 4;
-constexpr int kLoadsDone = 0x0F70;                 // s_waitcnt: no load or store on its way, whatever else is
 // Workgroups on a compute unit, by what LDS and registers give.
-constexpr int groups_at_once(int dt, int ap, int ct) { return ap > 128 || (dt != kBF16 && ap > 64) || (dt == kF16 && ct > 1) ? 1 : 2; }
+constexpr int groups_at_once(int ap) { return ap > 128 ? 1 : 2; }
+// s_waitcnt: no more than n loads and stores on their way, whatever else is.
+constexpr int loads_left(int n) { return (n & 15) | (n >> 4) << 14 | 0x0F70; }
 
 template <int N> struct Parts { bf16x8 p[N]; };
 
@@ -204,7 +207,7 @@ template <int COLS> __device__ __forceinline__ bf16x8 column_operand(const bf16_
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 // Keeps the compiler from computing what depends on v ahead of a loop: addresses made of a lane's number and constants would take dozens of registers.
-__device__ __forceinline__ int here(int v)
+template <class T> __device__ __forceinline__ T here(T v)
 {
     asm volatile("" : "+v"(v));
     return v;
@@ -227,6 +230,7 @@ template <int DT, int C, int COLS, int THREADS, bool WHOLE> struct Stage {
     static_assert(THREADS % (COLS / 8) == 0, "a lane keeps to its columns");
     static constexpr int kOffsets = kRowsAtOnce % 16 == 0 ? 1 : 2;             // the swizzle repeats every 16 rows
     static_assert(kRowsAtOnce % 8 == 0, "or every second time");
+    static constexpr int kSure = kItems / THREADS;             // loads that every wavefront makes of a block
     u32x4 v[kWay == kStaged ? kEach : 1][kQuads];
     const T *first;                                // the block's first row (the same for all lanes)
     long long step;                                // from row to row
@@ -358,38 +362,97 @@ template <class T, bool WHOLE, int K> __device__ __forceinline__ void store_colu
     }
 }
 
-// Calls what(element, its index) for the lane's elements of a state that exist.  The lane's number passes through an empty asm statement: otherwise
-// the compiler keeps every element's address and predicate from the reading of a state to its writing, registers that the walk needs.
-template <int AP, int CT, class What> __device__ __forceinline__ void each_of_state(f32x4 (&M)[AP / 16][CT], bool any, unsigned first_e, unsigned A, unsigned E, size_t m_a,
-                                                                                    size_t m_e, What what)
+// How a state lies in the registers of a workgroup, and between segments in memory: M[t][c][r] of thread `tid` is M[a][e] with
+//   a = 32 (t / 2) + 8 g + 4 (t % 2) + r,  e = 64 CT block + 16 CT wave + 4 CT (l / 4) + 4 c + l % 4,  tid = 64 wave + 16 g + l.
+// Four lanes side by side and r make 4 x 4 squares, so the transposed state lies likewise.  In memory: [block][t][c][tid][r].
+struct StateShape {
+    unsigned AP, CT;                               // A and E are padded to these multiples
+    __host__ __device__ unsigned columns() const { return 64 * CT; }
+    __host__ __device__ unsigned floats(unsigned E) const { return AP * ((E + columns() - 1) / columns()) * columns(); }
+    __device__ __forceinline__ void element(unsigned quad, unsigned &a0, unsigned &e) const        // of the quad-th four elements: (a0 + r, e)
+    {
+        const unsigned tid = quad % 256, c = quad / 256 % CT, t = quad / 256 / CT % (AP / 16), block = quad / 16 / AP / CT;
+        a0 = 32 * (t / 2) + 8 * (tid / 16 % 4) + 4 * (t % 2);
+        e = columns() * block + 16 * CT * (tid / 64) + 4 * CT * (tid / 4 % 4) + 4 * c + tid % 4;
+    }
+    __device__ __forceinline__ unsigned quad(unsigned a0, unsigned e) const
+    {
+        const unsigned block = e / columns(), x = e % columns(), wave = x / (16 * CT), y = x % (16 * CT), c = y / 4 % CT;
+        const unsigned tid = 64 * wave + 16 * (a0 / 8 % 4) + 4 * (y / (4 * CT)) + x % 4, t = 2 * (a0 / 32) + a0 / 4 % 2;
+        return ((block * (AP / 16) + t) * CT + c) * 256 + tid;
+    }
+};
+// (a workgroup's share of the registers: 256 rows of a state and 32 columns to a wavefront do not fit them)
+__host__ __device__ inline StateShape state_shape(unsigned A, unsigned E) { return {A <= 32 ? 32u : A <= 64 ? 64u : A <= 128 ? 128u : 256u, E <= 64 || A > 128 ? 1u : 2u}; }
+
+// The 4 x 4 square that four lanes side by side hold, transposed.
+__device__ __forceinline__ f32x4 turned(f32x4 v, int lane)
 {
-    unsigned lane = threadIdx.x & 63;
-    asm volatile("" : "+v"(lane));
-    if (!any) return;
-    const unsigned a0 = 8 * (lane >> 4), e_lane = first_e + 4 * CT * ((lane & 15) >> 2) + (lane & 3);
+    auto from = [](float x, auto how) { return bits<float>((uint32_t)__builtin_amdgcn_mov_dpp((int)bits<uint32_t>(x), decltype(how)::value, 0xf, 0xf, true)); };
+    typedef std::integral_constant<int, kQuadPerm1032> Next;
+    typedef std::integral_constant<int, kQuadPerm2301> Across;
+    const bool odd = lane & 1, high = lane & 2;
+    const float a = from(odd ? v[0] : v[1], Next()), b = from(odd ? v[2] : v[3], Next());
+    v = odd ? f32x4{a, v[1], b, v[3]} : f32x4{v[0], a, v[2], b};
+    const float c = from(high ? v[0] : v[2], Across()), d = from(high ? v[1] : v[3], Across());
+    return high ? f32x4{c, d, v[2], v[3]} : f32x4{v[0], v[1], c, d};
+}
+// A caller's state into the registers or out of them: M[a][e] at p[a * m_a + e * m_e].  16 bytes at a time where rows or columns are dense.  The lane's number
+// passes through an empty asm statement: otherwise the compiler keeps every address and predicate from the reading of a state to its writing.
+template <int AP, int CT, bool OUT, class P> __device__ __forceinline__ void move_state(f32x4 (&M)[AP / 16][CT], P *p, unsigned first_e, unsigned A, unsigned E, size_t m_a, size_t m_e)
+{
+    const unsigned lane = here(threadIdx.x & 63), a0 = 8 * (lane >> 4), s = lane & 3, e_lane = first_e + 4 * CT * ((lane & 15) >> 2) + s;
+    typedef std::conditional_t<OUT, f32x4, const f32x4> Quad;
+    const bool rows = m_e == 1 && E % 4 == 0, columns = m_a == 1 && A % 4 == 0;
 #pragma unroll
     for (int t = 0; t < AP / 16; ++t)
 #pragma unroll
-        for (int c = 0; c < CT; ++c)
+        for (int c = 0; c < CT; ++c) {
+            const unsigned a = a0 + 32 * (t / 2) + 4 * (t & 1), e = e_lane + 4 * c;
+            if (rows) {
+                Quad *q = (Quad *)(p + (size_t)(a + s) * m_a + (e - s));
+                f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+                const bool there = a + s < A && e < E;
+                if constexpr (OUT) {
+                    v = turned(M[t][c], lane);
+                    if (there) *q = v;
+                } else {
+                    if (there) v = *q;
+                    M[t][c] = turned(v, lane);
+                }
+            } else if (columns) {
+                Quad *q = (Quad *)(p + a + (size_t)e * m_e);
+                if (a < A && e < E) {
+                    if constexpr (OUT) *q = M[t][c];
+                    else M[t][c] = *q;
+                }
+            } else {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const unsigned a = a0 + 32 * (t / 2) + 4 * (t & 1) + r, e = e_lane + 4 * c;
-                float m = M[t][c][r];
-                if (a < A && e < E) what(m, a * m_a + e * m_e);
-                M[t][c][r] = m;
+                for (int r = 0; r < 4; ++r)
+                    if (a + r < A && e < E) {
+                        if constexpr (OUT) p[(a + r) * m_a + e * m_e] = M[t][c][r];
+                        else M[t][c][r] = p[(a + r) * m_a + e * m_e];
+                    }
             }
+        }
 }
 
 // READS: writes outputs and, of a row's last segment, the state.  Otherwise only what each segment but the last adds to the state.
-template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bounds__(64 * kWalkWaves, groups_at_once(DT, AP, CT)) void walk_kernel(WalkArgs W)
+template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bounds__(64 * kWalkWaves, groups_at_once(AP)) void walk_kernel(WalkArgs W)
 {
     typedef typename Elem<DT>::T T;
-    constexpr int N = parts_of(DT), C = block_tokens(DT, AP), EB = 16 * kWalkWaves * CT, kThreads = 64 * kWalkWaves;
+    constexpr int N = parts_of(DT), C = kBlock, EB = 16 * kWalkWaves * CT, kThreads = 64 * kWalkWaves;
     constexpr bool kDirectly = way_of(DT, WHOLE) == kDirect;
-    constexpr int kTiles = C / 16, kSteps = C / 32, kOrder = N == 3 ? 3 : 2;       // tiles of 16 tokens, steps of 32
-    __shared__ __attribute__((aligned(16))) bf16_t sy[N * C * AP], sz[N * C * EB], sx[READS ? N * C * AP : 8], sp[READS ? N * C * C : 8];
-    // (arrays of their own: loads into the one are not waited for to read the other)
-    __shared__ __attribute__((aligned(16))) bf16_t sy_too[kDirectly ? C * AP : 8], sz_too[kDirectly && !READS ? C * EB : 8];
+    constexpr int kTiles = C / 16, kOrder = N == 3 ? 3 : 2;    // tiles of 16 tokens
+    typedef Stage<DT, C, AP, kThreads, WHOLE> StageA;
+    typedef Stage<DT, C, EB, kThreads, WHOLE> StageE;
+    // Loads that write LDS themselves go round kRing tiles of each array: while a block is worked on, the kRing - 1 behind it are on their way.
+    constexpr int kRing = !kDirectly ? 1 : READS ? 3 : 4, kLoads = (READS ? 2 : 1) * StageA::kSure + StageE::kSure;
+    // (Each tile is an array of its own: the compiler has a wavefront wait for loads into an array before it reads from it.)
+    constexpr int kX = READS ? N * C * AP : 8, kY = N * C * AP, kZ = N * C * EB, kNone = 8;
+    __shared__ __attribute__((aligned(16))) bf16_t sx0[kX], sx1[kRing > 1 ? kX : kNone], sx2[kRing > 2 ? kX : kNone], sp[READS ? N * C * C : kNone];
+    __shared__ __attribute__((aligned(16))) bf16_t sy0[kY], sy1[kRing > 1 ? kY : kNone], sy2[kRing > 2 ? kY : kNone], sy3[kRing > 3 ? kY : kNone];
+    __shared__ __attribute__((aligned(16))) bf16_t sz0[kZ], sz1[kRing > 1 ? kZ : kNone], sz2[kRing > 2 ? kZ : kNone], sz3[kRing > 3 ? kZ : kNone];
 
     const unsigned blocks = (W.E + EB - 1) / EB;
     const unsigned block = blockIdx.x % blocks, h = blockIdx.x / blocks % W.heads, number = blockIdx.x / blocks / W.heads;
@@ -407,30 +470,31 @@ template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bo
     const float log_decay = W.log_decay[h];
     const int e0 = (int)block * EB, wave_e = 16 * CT * wave;        // the workgroup's first column, and the wavefront's of these
     const long long slot = state_of(W.slots, piece.r, W.states);
-    const size_t state = ((size_t)slot * W.heads + h) * W.A * W.E, between = ((size_t)number * W.heads + h) * W.A * W.E;
+    const size_t state = ((size_t)slot * W.heads + h) * W.A * W.E;
+    f32x4 *between = (f32x4 *)W.between + (((size_t)number * W.heads + h) * blocks + block) * (AP * EB / 4) + threadIdx.x;
     const bool cut = piece.first > 0 || !piece.last;                // a row of several segments
-    // M[2 s + t][c][r] is M[a][e] with a = 32 s + 8 g + 4 t + r, e = e0 + wave_e + 4 CT (l / 4) + 4 c + l % 4: the columns of a lane's outputs are
-    // then next to each other
     f32x4 M[AP / 16][CT] = {};
-    {
+    if constexpr (READS) {
         // a row of several segments finds what it starts from in the workspace, also for the first of them
-        const float *from = !READS ? nullptr : cut ? W.between + between : W.m_in && slot >= 0 ? W.m_in + state : nullptr;
-        const size_t m_a = cut ? W.between_a : W.m_a, m_e = cut ? W.between_e : W.m_e;
-        each_of_state<AP, CT>(M, from != nullptr, e0 + wave_e, W.A, W.E, m_a, m_e, [&](float &m, size_t i) { m = from[i]; });
+        if (cut)
+#pragma unroll
+            for (int t = 0; t < AP / 16; ++t)
+#pragma unroll
+                for (int c = 0; c < CT; ++c) M[t][c] = between[(t * CT + c) * 256];
+        else if (W.m_in && slot >= 0)
+            move_state<AP, CT, false>(M, W.m_in + state, e0 + wave_e, W.A, W.E, W.m_a, W.m_e);
     }
     float reading[kTiles];                         // by_read a^(i+1), from the end a^i, of the lane's token in each tile
     const float by_key = W.by_read * W.by_new;
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) reading[t] = W.by_read * decay_power(log_decay, (float)(16 * t + l + (W.from_end ? 0 : 1)));
     if (READS)                                     // P above its diagonal of tiles: zeros for good
-        for (int i = threadIdx.x; i < N * (C / 32) * 16 * 2; i += kThreads) {
-            const int n = i / (C / 32 * 32), t = i / 32 % (C / 32), row = i / 2 % 16, half = i % 2;
-            *(u32x4 *)(sp + n * C * C + Tile<C>::at(32 * t + row, 32 * t + 16 + 8 * half)) = u32x4{0u, 0u, 0u, 0u};
-        }
+        for (int i = threadIdx.x; i < N * 32; i += kThreads)
+            *(u32x4 *)(sp + i / 32 * C * C + Tile<C>::at(i / 2 % 16, 16 + 8 * (i % 2))) = u32x4{0u, 0u, 0u, 0u};
 
     const long long sign = W.from_end ? -1 : 1, origin = (W.from_end ? piece.hi - 1 : piece.lo) + sign * piece.first;
-    Stage<DT, C, AP, kThreads, WHOLE> next_x, next_y;
-    Stage<DT, C, EB, kThreads, WHOLE> next_z;
+    StageA next_x, next_y;
+    StageE next_z;
     next_x.begin((const T *)W.x.data + W.x.at(h, W.heads) + origin * W.x.token, sign * W.x.token, (int)W.A);
     next_y.begin((const T *)W.y.data + W.y.at(h, W.heads) + origin * W.y.token, sign * W.y.token, (int)W.A);
     next_z.begin((const T *)W.z.data + W.z.at(h, W.heads) + origin * W.z.token + e0, sign * W.z.token, (int)W.E - e0);
@@ -440,141 +504,104 @@ template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bo
     char *out = (char *)W.out.data + (W.out.at(h, W.heads) + origin * W.out.token) * out_size + (sign < 0 ? 15 * out_step : 0);
     typedef std::conditional_t<WHOLE, unsigned, long long> Offset;
     const Offset out_lane = (Offset)((sign < 0 ? l - 15 : l) * out_step) + (Offset)(col * out_size);         // (not negative: outputs have positive strides)
-    float *to = !READS ? W.between + between : piece.last && W.m_out && slot >= 0 ? W.m_out + state : nullptr;
-    // the third part of what is added to a state counts where the state itself is asked for, not where 16-bit outputs are read from it
-    constexpr int kParts = !READS || N == 3 ? 3 : 2;
-    const bool exact = to != nullptr;
+    // The third part of what is added to a state counts where the state itself is asked for, not where 16-bit outputs are read from it; and there for the tokens
+    // of which more than an eighth is left at the end of the row (the two parts are 3e-6 off: less than the last bits of fp32 sums then).
+    constexpr int kParts = N == 3 ? 3 : 2;
+    const bool exact = W.m_out && slot >= 0 && decay_power(log_decay, (float)(piece.hi - piece.lo - piece.end)) > 0.125f;
     const long long length = piece.end - piece.first;
-    // Loads of the next block start as soon as their tiles in LDS are free, a part of the work apart: more of them at once than the memory
-    // pipeline takes hold up the wavefront.
     auto tokens = [&](long long left) { return (int)(left < C ? left : C); };
-    f32x8 weight[kSteps];                          // by_new a^(n-1-j), from the end a^(n-j), of the lane's tokens j of each step
-    auto set_weights = [&](int n) {
+    // by_new a^(n-1-j), from the end a^(n-j), of the lane's tokens j = 8 g + k: in whole blocks a power for the lane's group times one for k, which is the
+    // same for all lanes
+    const float group_power = W.by_new * decay_power(log_decay, (float)(C - 8 - 8 * g + (W.from_end ? 1 : 0)));
+    float near_power[8];
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s)
+    for (int k = 0; k < 8; ++k) near_power[k] = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, decay_power(log_decay, (float)(7 - k)))));
+    auto weights = [&](int n) {
+        f32x8 w;
+        if (n == C) {
+            const float far = here(group_power);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) w[k] = far * near_power[k];
+        } else {
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const int j = 32 * s + 8 * g + k;
-                weight[s][k] = j < n ? W.by_new * decay_power(log_decay, (float)(n - 1 - j + (W.from_end ? 1 : 0))) : 0.0f;
+                const int j = here(8 * g) + k;
+                w[k] = j < n ? W.by_new * decay_power(log_decay, (float)(n - 1 - j + (W.from_end ? 1 : 0))) : 0.0f;
             }
+        }
+        return w;
     };
-    if (length > 0) {
-        if constexpr (READS) next_x.load(sx, tokens(length));
-        next_y.load(sy, tokens(length));
-        next_z.load(sz, tokens(length));
-    }
-    set_weights(tokens(length));
+    long long left = length;                       // tokens that are not on their way yet
+    auto load = [&](bf16_t *x_tile, bf16_t *y_tile, bf16_t *z_tile) {
+        if (left <= 0) return;
+        const int n = tokens(left);
+        if constexpr (READS) next_x.load(x_tile, n);
+        next_y.load(y_tile, n);
+        next_z.load(z_tile, n);
+        left -= C;
+    };
+    load(sx0, sy0, sz0);
+    if constexpr (kRing > 2) load(sx1, sy1, sz1);
+    if constexpr (kRing > 3) load(sx2, sy2, sz2);
     Decays whole_block(log_decay, (float)C);
     long long at = 0;
-    // (Y has two tiles in LDS if loads write there themselves, Z only where there are no outputs)
-    auto take_block = [&](bf16_t *const y_now, bf16_t *const y_next, bf16_t *const z_now, bf16_t *const z_next) __attribute__((always_inline)) {
+    // A block in the tiles `now`; behind the barrier, the tiles of the block before are free to be loaded into.
+    auto take_block = [&](bf16_t *x_now, bf16_t *x_free, bf16_t *y_now, bf16_t *y_free, bf16_t *z_now, bf16_t *z_free) __attribute__((always_inline)) {
+        const long long behind = length - at - C;
         const int n = tokens(length - at);
-        const long long left = length - at - C;                // behind this block
         const int row_at = here(row_lane<AP>(lane)), p_at = here(row_lane<C>(lane)), y_at = here(column_lane<AP, 8>(lane, 0)), z_at = here(column_lane<EB, 4 * CT>(lane, wave_e));
         if constexpr (kDirectly) {
-            __builtin_amdgcn_s_waitcnt(kLoadsDone);
+            // of the loads behind this block's, as many may be on their way as there surely are (stores are waited for with them)
+            if (kRing > 3 && behind > C) __builtin_amdgcn_s_waitcnt(loads_left((kRing > 3 ? 2 : 1) * kLoads));
+            else if (behind > 0) __builtin_amdgcn_s_waitcnt(loads_left(kLoads));
+            else __builtin_amdgcn_s_waitcnt(loads_left(0));
         } else {
             __syncthreads();                       // everybody has done with the block before
-            if constexpr (READS) next_x.store(sx, n);
-            next_y.store(sy, n);
-            next_z.store(sz, n);
+            if constexpr (READS) next_x.store(x_now, n);
+            next_y.store(y_now, n);
+            next_z.store(z_now, n);
         }
         __syncthreads();
-        if (kDirectly && left > 0) {
-            next_y.load(y_next, tokens(left));
-            if constexpr (!READS) next_z.load(z_next, tokens(left));
-        }
-        if (n < C && at > 0) set_weights(n);
+        if constexpr (kDirectly) load(x_free, y_free, z_free);
         if constexpr (READS) {
-            // P^T, 16 keys by 16 queries at a time.  Of the ten tiles on and below the diagonal each wavefront takes two or three that share operands:
-            // queries' tile 3 with keys' 0 and 1 | 3 with 2 and 3 | 2 with 0, 1 and 2 | 1 with 0 and 1, 0 with 0; of three: 0 with 0 | 1 with 0 | 1 with 1 | none
-            constexpr int kMine = kTiles == 4 ? 3 : 1;
-            const int mine = kTiles == 4 ? wave < 2 ? 2 : 3 : wave < 3 ? 1 : 0;
-            int it[kMine], jt[kMine];
-#pragma unroll
-            for (int k = 0; k < kMine; ++k) {
-                it[k] = kTiles == 4 ? wave < 2 ? 3 : wave == 2 ? 2 : k < 2 ? 1 : 0 : wave > 0 ? 1 : 0;
-                jt[k] = kTiles == 4 ? wave == 1 ? 2 + (k & 1) : wave == 3 ? k & 1 : k : wave == 2 ? 1 : 0;
-            }
-            f32x4 p[kMine];
-#pragma unroll
-            for (int k = 0; k < kMine; ++k) p[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int s = 0; s < AP / 32; ++s) {
-                Parts<N> keys[kMine], queries;
-#pragma unroll
-                for (int m = 0; m < N; ++m) {
-                    queries.p[m] = row_operand<AP>(sx + m * C * AP, row_at, 16 * it[0], 32 * s);
-#pragma unroll
-                    for (int k = 0; k < (kMine < 2 ? kMine : 2); ++k) keys[k].p[m] = row_operand<AP>(y_now + m * C * AP, row_at, 16 * jt[k], 32 * s);
-                }
-                products<kOrder>([&](int i, int j) {
-#pragma unroll
-                    for (int k = 0; k < (kMine < 2 ? kMine : 2); ++k) p[k] = mfma(keys[k].p[i], queries.p[j], p[k]);
-                }, keys[0], queries);
-            }
-            if (kMine > 2 && mine > 2)
+            // P^T, 16 keys by 16 queries at a time: three of the wavefronts have a tile on or below the diagonal
+            if (wave < 3) {
+                const int it = wave > 0, jt = wave > 1;
+                f32x4 p = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int s = 0; s < AP / 32; ++s) {
                     Parts<N> keys, queries;
 #pragma unroll
                     for (int m = 0; m < N; ++m) {
-                        queries.p[m] = row_operand<AP>(sx + m * C * AP, row_at, 16 * it[kMine - 1], 32 * s);
-                        keys.p[m] = row_operand<AP>(y_now + m * C * AP, row_at, 16 * jt[kMine - 1], 32 * s);
+                        keys.p[m] = row_operand<AP>(y_now + m * C * AP, row_at, 16 * jt, 32 * s);
+                        queries.p[m] = row_operand<AP>(x_now + m * C * AP, row_at, 16 * it, 32 * s);
                     }
-                    products<kOrder>([&](int i, int j) { p[kMine - 1] = mfma(keys.p[i], queries.p[j], p[kMine - 1]); }, keys, queries);
+                    products<kOrder>([&](int i, int j) { p = mfma(keys.p[i], queries.p[j], p); }, keys, queries);
                 }
+                const int i = 16 * it + l, j = 16 * jt + 4 * g, apart = here(i - j);
 #pragma unroll
-            for (int k = 0; k < kMine; ++k) {
-                if (k >= mine) break;
-                const int i = 16 * it[k] + l, j = 16 * jt[k] + 4 * g, apart = here(i - j);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) p[k][r] = apart >= r ? p[k][r] * (by_key * decay_power(log_decay, (float)(apart - r))) : 0.0f;
+                for (int r = 0; r < 4; ++r) p[r] = apart >= r ? p[r] * (by_key * decay_power(log_decay, (float)(apart - r))) : 0.0f;
 #pragma unroll
                 for (int m = 0; m < N; ++m) {
-                    const bf16x4 part = __builtin_convertvector(p[k], bf16x4);
+                    const bf16x4 part = __builtin_convertvector(p, bf16x4);
                     *(bf16x4 *)(sp + m * C * C + Tile<C>::at(i, j)) = part;
-                    p[k] -= __builtin_convertvector(part, f32x4);
+                    p -= __builtin_convertvector(part, f32x4);
                 }
             }
             __syncthreads();
         }
-        Parts<N> zt[kSteps][CT];                   // 16 columns of Z by 32 tokens
+        Parts<N> zt[CT];                           // 16 columns of Z by 32 tokens
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s)
+        for (int c = 0; c < CT; ++c)
 #pragma unroll
-            for (int c = 0; c < CT; ++c)
+            for (int m = 0; m < N; ++m) zt[c].p[m] = column_operand<EB>(z_now + m * C * EB, z_at, 0, 4 * c);
+        // what is added to the state
+        const f32x8 w = weights(n);
+        auto weighted = [&](int c) {
+            f32x8 v = __builtin_convertvector(zt[c].p[N - 1], f32x8);
 #pragma unroll
-                for (int m = 0; m < N; ++m) zt[s][c].p[m] = column_operand<EB>(z_now + m * C * EB, z_at, 32 * s, 4 * c);
-        auto whole_z = [&](int s, int c) {
-            f32x8 v = __builtin_convertvector(zt[s][c].p[N - 1], f32x8);
-#pragma unroll
-            for (int m = N - 2; m >= 0; --m) v += __builtin_convertvector(zt[s][c].p[m], f32x8);
-            return v;
-        };
-        Parts<kParts> wz[2][CT];                   // what is added to the state, of this step of 32 tokens and of the next
-        auto weigh = [&](int s) {
-#pragma unroll
-            for (int c = 0; c < CT; ++c) wz[s & 1][c] = split<kParts>(whole_z(s, c) * weight[s]);
-        };
-        // the state decays and the first step is weighted next to other products
-        auto begin_update = [&] {
-            weigh(0);
-            const float by = n == C ? whole_block.by() : Decays(log_decay, (float)n).by();
-#pragma unroll
-            for (int t = 0; t < AP / 16; ++t)
-#pragma unroll
-                for (int c = 0; c < CT; ++c) M[t][c] *= by;
-            if constexpr (READS) {                 // (here, where products run that need nothing of it, and not where it is used)
-#pragma unroll
-                for (int c = 0; c < CT; ++c)
-#pragma unroll
-                    for (int i = 0; i < kParts; ++i) asm volatile("" : "+v"(wz[0][c].p[i]));
-#pragma unroll
-                for (int t = 0; t < AP / 16; ++t)
-#pragma unroll
-                    for (int c = 0; c < CT; ++c) asm volatile("" : "+v"(M[t][c]));
-            }
+            for (int m = N - 2; m >= 0; --m) v += __builtin_convertvector(zt[c].p[m], f32x8);
+            return v * w;
         };
         constexpr int NM = N == 3 ? 3 : 2;
         f32x4 o[kTiles][CT];
@@ -596,9 +623,8 @@ template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bo
 #pragma unroll
                 for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-                    for (int i = 0; i < N; ++i) b[t].p[i] = row_operand<AP>(sx + i * C * AP, row_at, 16 * t, 32 * s);
+                    for (int i = 0; i < N; ++i) b[t].p[i] = row_operand<AP>(x_now + i * C * AP, row_at, 16 * t, 32 * s);
                 if (s + 1 < AP / 32) split_m(s + 1);
-                else begin_update();
                 products<kOrder>([&](int i, int j) {           // (independent ones behind each other)
 #pragma unroll
                     for (int c = 0; c < CT; ++c)
@@ -607,28 +633,22 @@ template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bo
                 }, m[0][0], b[0]);
             }
         }
-        __builtin_amdgcn_sched_barrier(0);
         if constexpr (READS) {
-            if constexpr (kDirectly) __syncthreads();          // (X and Z have been read)
-            if (left > 0) next_x.load(sx, tokens(left));
 #pragma unroll
             for (int t = 0; t < kTiles; ++t)
 #pragma unroll
                 for (int c = 0; c < CT; ++c) o[t][c] *= reading[t];
+            Parts<N> b[kTiles];
 #pragma unroll
-            for (int s = 0; s < kSteps; ++s) {
-                Parts<N> b[kTiles];
+            for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-                for (int t = 2 * s; t < kTiles; ++t)
+                for (int i = 0; i < N; ++i) b[t].p[i] = row_operand<C>(sp + i * C * C, p_at, 16 * t, 0);
+            products<kOrder>([&](int i, int j) {
 #pragma unroll
-                    for (int i = 0; i < N; ++i) b[t].p[i] = row_operand<C>(sp + i * C * C, p_at, 16 * t, 32 * s);
-                products<kOrder>([&](int i, int j) {
+                for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-                    for (int t = 2 * s; t < kTiles; ++t)
-#pragma unroll
-                        for (int c = 0; c < CT; ++c) o[t][c] = mfma(zt[s][c].p[i], b[t].p[j], o[t][c]);
-                }, zt[0][0], b[0]);
-            }
+                    for (int c = 0; c < CT; ++c) o[t][c] = mfma(zt[c].p[i], b[t].p[j], o[t][c]);
+            }, zt[0], b[0]);
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) {
                 if (16 * t + l >= n) continue;
@@ -638,83 +658,117 @@ template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bo
             }
             out += C * out_step;
         }
-        if constexpr (!READS) begin_update();
-        if ((READS || !kDirectly) && left > 0) next_z.load(sz, tokens(left));
-        if (!kDirectly && left > 0) next_y.load(sy, tokens(left));
+        if constexpr (!kDirectly) load(x_now, y_now, z_now);   // (as far as the registers)
+        // the state
+        const float by = n == C ? whole_block.by() : Decays(log_decay, (float)n).by();
+        Parts<kParts> wz[CT];
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            __builtin_amdgcn_sched_barrier(0);
-            Parts<N> yt[2][2];                     // two tiles of M's rows, and the next two
-            auto load_y = [&](int t) {
+        for (int c = 0; c < CT; ++c) wz[c] = split<kParts>(weighted(c));
+        Parts<N> yt[2][2];                         // two tiles of M's rows, and the next two
+        auto load_y = [&](int t) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int m = 0; m < N; ++m) yt[t / 2 & 1][u].p[m] = column_operand<AP>(y_now + m * C * AP, y_at, 0, 16 * t + 4 * u);
+        };
+        load_y(0);
+#pragma unroll
+        for (int t = 0; t < AP / 16; t += 2) {
+            if (t + 2 < AP / 16) load_y(t + 2);
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int c = 0; c < CT; ++c) M[t + u][c] *= by;
+            products<kParts>([&](int i, int j) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
 #pragma unroll
-                    for (int m = 0; m < N; ++m) yt[t / 2 & 1][u].p[m] = column_operand<AP>(y_now + m * C * AP, y_at, 32 * s, 16 * t + 4 * u);
-            };
-            load_y(0);
-#pragma unroll
-            for (int t = 0; t < AP / 16; t += 2) {
-                if (t + 2 < AP / 16) load_y(t + 2);
-                products<kParts>([&](int i, int j) {
-#pragma unroll
-                    for (int u = 0; u < 2; ++u)
-#pragma unroll
-                        for (int c = 0; c < CT; ++c) M[t + u][c] = mfma(yt[t / 2 & 1][u].p[i], wz[s & 1][c].p[j], M[t + u][c]);
-                }, yt[0][0], wz[0][0]);
-            }
-            if (s + 1 < kSteps) weigh(s + 1);
+                    for (int c = 0; c < CT; ++c) M[t + u][c] = mfma(yt[t / 2 & 1][u].p[i], wz[c].p[j], M[t + u][c]);
+            }, yt[0][0], wz[0]);
         }
         if constexpr (kParts == 2)
-            if (exact)                             // the third parts
+            if (exact) {                           // the third parts
+                Parts<3> third[CT];
 #pragma unroll
-                for (int s = 0; s < kSteps; ++s) {
-                    Parts<3> third[CT];
+                for (int c = 0; c < CT; ++c) third[c] = split<3>(weighted(c));
 #pragma unroll
-                    for (int c = 0; c < CT; ++c) third[c] = split<3>(whole_z(s, c) * weight[s]);
+                for (int t = 0; t < AP / 16; ++t)
 #pragma unroll
-                    for (int t = 0; t < AP / 16; ++t)
+                    for (int m = 0; m < N; ++m) {
+                        const bf16x8 y_part = column_operand<AP>(y_now + m * C * AP, y_at, 0, 32 * (t / 2) + 4 * (t & 1));
 #pragma unroll
-                        for (int m = 0; m < N; ++m) {
-                            const bf16x8 yt = column_operand<AP>(y_now + m * C * AP, y_at, 32 * s, 32 * (t / 2) + 4 * (t & 1));
-#pragma unroll
-                            for (int c = 0; c < CT; ++c) M[t][c] = mfma(yt, third[c].p[2 - m], M[t][c]);
-                        }
-                }
+                        for (int c = 0; c < CT; ++c) M[t][c] = mfma(y_part, third[c].p[2 - m], M[t][c]);
+                    }
+            }
         at += C;
     };
-    while (at < length) {
-        take_block(sy, sy_too, sz, sz_too);
-        if (kDirectly && at < length) take_block(sy_too, sy, READS ? sz : sz_too, sz);
+    if constexpr (kRing == 4) {
+        while (at < length) {
+            take_block(sx0, sx0, sy0, sy3, sz0, sz3);
+            if (at < length) take_block(sx0, sx0, sy1, sy0, sz1, sz0);
+            if (at < length) take_block(sx0, sx0, sy2, sy1, sz2, sz1);
+            if (at < length) take_block(sx0, sx0, sy3, sy2, sz3, sz2);
+        }
+    } else if constexpr (kRing == 3) {
+        while (at < length) {
+            take_block(sx0, sx2, sy0, sy2, sz0, sz2);
+            if (at < length) take_block(sx1, sx0, sy1, sy0, sz1, sz0);
+            if (at < length) take_block(sx2, sx1, sy2, sy1, sz2, sz1);
+        }
+    } else {
+        while (at < length) take_block(sx0, sx0, sy0, sy0, sz0, sz0);
     }
-    const size_t m_a = READS ? W.m_a : W.between_a, m_e = READS ? W.m_e : W.between_e;
-    each_of_state<AP, CT>(M, to != nullptr, e0 + wave_e, W.A, W.E, m_a, m_e, [&](float &m, size_t i) { to[i] = m; });
+    if constexpr (!READS) {
+#pragma unroll
+        for (int t = 0; t < AP / 16; ++t)
+#pragma unroll
+            for (int c = 0; c < CT; ++c) between[(t * CT + c) * 256] = M[t][c];
+    } else if (piece.last && W.m_out && slot >= 0) {
+        move_state<AP, CT, true>(M, W.m_out + state, e0 + wave_e, W.A, W.E, W.m_a, W.m_e);
+    }
 }
 
-// What each segment of a row starts from, from what the segments in front of it add: a thread takes one element of the state along the row.
-constexpr int kJoinThreads = 256, kJoinAhead = 8;
+// What each segment of a row starts from, from what the segments in front of it add: a thread takes four elements of the state along the row.
+constexpr int kJoinThreads = 256, kJoinAhead = 4;
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(WalkArgs W)
 {
-    const unsigned size = W.A * W.E, blocks = (size + kJoinThreads - 1) / kJoinThreads;
-    const unsigned i = blockIdx.x % blocks * kJoinThreads + threadIdx.x, h = blockIdx.x / blocks % W.heads, r = blockIdx.x / blocks / W.heads;
-    if (i >= size) return;
+    const StateShape shape = state_shape(W.A, W.E), turned_shape = state_shape(W.E, W.A);
+    const unsigned quads = shape.floats(W.E) / 4, turned_quads = turned_shape.floats(W.A) / 4, blocks = quads / kJoinThreads;
+    const unsigned i = blockIdx.x % blocks * kJoinThreads + threadIdx.x, h = blockIdx.x / blocks % W.heads, row = blockIdx.x / blocks / W.heads;
     long long lo, hi;
-    row_extent(W.offsets, r, W.total, lo, hi);
-    const long long segment = 1ll << W.segment_log2, segments = (hi - lo + segment - 1) >> W.segment_log2, first = (lo >> W.segment_log2) + r;
+    row_extent(W.offsets, row, W.total, lo, hi);
+    const long long segment = 1ll << W.segment_log2, segments = (hi - lo + segment - 1) >> W.segment_log2, first = (lo >> W.segment_log2) + row;
     if (segments <= 1 || first + segments > (long long)W.pieces) return;
-    const long long slot = state_of(W.slots, r, W.states);
-    const unsigned a = W.between_e == 1 ? i / W.E : i % W.A, e = W.between_e == 1 ? i % W.E : i / W.A;         // element i of a state between segments
-    float m = W.m_in && slot >= 0 ? W.m_in[((size_t)slot * W.heads + h) * size + (size_t)a * W.m_a + (size_t)e * W.m_e] : 0.0f;
-    const Decay decay(W.log_decay[h], (float)segment);
-    float *p = W.between + ((size_t)first * W.heads + h) * size + i;
-    const size_t step = (size_t)W.heads * size;
-    for (long long s = 0; s < segments; s += kJoinAhead) {
-        float added[kJoinAhead];                   // (of the last segment nothing is known, nor asked for)
+    const long long slot = state_of(W.slots, row, W.states);
+    unsigned a0, e;
+    shape.element(i, a0, e);
+    f32x4 m = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (W.m_in && slot >= 0)
 #pragma unroll
-        for (int u = 0; u < kJoinAhead; ++u) added[u] = s + u + 1 < segments ? p[(s + u) * step] : 0.0f;
+        for (int r = 0; r < 4; ++r)
+            if (a0 + r < W.A && e < W.E) m[r] = W.m_in[((size_t)slot * W.heads + h) * W.A * W.E + (size_t)(a0 + r) * W.m_a + (size_t)e * W.m_e];
+    const Decay decay(W.log_decay[h], (float)segment);
+    f32x4 *p = (f32x4 *)W.between + ((size_t)first * W.heads + h) * quads + i;
+    // of the transposed state, rows e .. and column a0 + r change places
+    const bool turn = W.between_turned && (e & ~3u) < turned_shape.AP && a0 < turned_quads * 4 / turned_shape.AP;
+    f32x4 *q = (f32x4 *)W.between_turned + ((size_t)first * W.heads + h) * turned_quads + (turn ? turned_shape.quad(e & ~3u, a0 + (threadIdx.x & 3)) : 0);
+    const size_t step = (size_t)W.heads * quads, turned_step = (size_t)W.heads * turned_quads;
+    for (long long s = 0; s < segments; s += kJoinAhead) {
+        f32x4 added[kJoinAhead];                   // (of the last segment nothing is known, nor asked for)
 #pragma unroll
         for (int u = 0; u < kJoinAhead; ++u) {
-            if (s + u < segments) p[(s + u) * step] = m;
-            m = decay(m) + added[u];
+            added[u] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            if (s + u + 1 < segments) added[u] = p[(s + u) * step];
+        }
+#pragma unroll
+        for (int u = 0; u < kJoinAhead; ++u) {
+            if (s + u < segments) {
+                p[(s + u) * step] = m;
+                const f32x4 across = turned(m, threadIdx.x);
+                if (turn) q[(s + u) * turned_step] = across;
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) m[r] = decay(m[r]) + added[u][r];
         }
     }
 }
@@ -862,14 +916,19 @@ unsigned segment_log2_for(const tcuscan_attention_shape_t &s)
 size_t pieces_for(const tcuscan_attention_shape_t &s, unsigned segment_log2) { return (size_t)s.rows + ((size_t)s.total >> segment_log2); }
 
 struct Layout {
-    size_t between, part, all;
+    size_t between, turned, part, all;
     unsigned segment_log2;
     Layout(const tcuscan_attention_shape_t &s, bool backward)
     {
         segment_log2 = segment_log2_for(s);
         between = chain_layout::kHeaderBytes;
-        part = between + (segment_log2 == kWholeRows ? 0 : pieces_for(s, segment_log2) * s.heads * s.dk * s.dv * 4);
-        part = (part + 255) / 256 * 256;
+        turned = part = between;
+        if (segment_log2 != kWholeRows) {
+            const size_t state = state_shape((unsigned)s.dk, (unsigned)s.dv).floats((unsigned)s.dv), other = state_shape((unsigned)s.dv, (unsigned)s.dk).floats((unsigned)s.dk);
+            const size_t all_states = pieces_for(s, segment_log2) * s.heads * 4;
+            turned = between + all_states * (backward && other > state ? other : state);
+            part = turned + (backward ? all_states * other : 0);
+        }
         size_t wide = 0;
         if (backward) {
             if (s.q_heads < s.heads || s.k_heads < s.heads) wide = (size_t)s.dk;
@@ -889,10 +948,10 @@ template <int DT, int CT, bool WHOLE, bool READS> const void *walk_for(unsigned 
          : A <= 128 ? (const void *)walk_kernel<DT, 128, CT, WHOLE, READS> : (const void *)walk_kernel<DT, 256, 1, WHOLE, READS>;
 }
 template <int DT, int CT, bool READS> const void *walk_for(unsigned A, bool whole) { return whole ? walk_for<DT, CT, true, READS>(A) : walk_for<DT, CT, false, READS>(A); }
-template <int DT, bool READS> const void *walk_for(unsigned A, bool whole, unsigned tiles) { return tiles == 1 ? walk_for<DT, 1, READS>(A, whole) : walk_for<DT, 2, READS>(A, whole); }
-template <bool READS> const void *walk_for(int dt, unsigned A, bool whole, unsigned tiles)
+template <int DT, bool READS> const void *walk_for(unsigned A, bool whole, unsigned CT) { return CT == 1 ? walk_for<DT, 1, READS>(A, whole) : walk_for<DT, 2, READS>(A, whole); }
+template <bool READS> const void *walk_for(int dt, unsigned A, bool whole, unsigned CT)
 {
-    return dt == kF16 ? walk_for<kF16, READS>(A, whole, tiles) : dt == kF32 ? walk_for<kF32, READS>(A, whole, tiles) : walk_for<kBF16, READS>(A, whole, tiles);
+    return dt == kF16 ? walk_for<kF16, READS>(A, whole, CT) : dt == kF32 ? walk_for<kF32, READS>(A, whole, CT) : walk_for<kBF16, READS>(A, whole, CT);
 }
 
 // Whether groups of eight elements of every token's features are aligned and whole, and 64 tokens within reach of a 32-bit offset.
@@ -902,25 +961,24 @@ bool whole(const Heads &x, unsigned dims, size_t esz)
            (x.token < 0 ? -x.token : x.token) < (1ll << 22);
 }
 
-// One walk, into `out`; with heads that share the output, into `part` first.  `states_ready`: a walk with the same states, or transposed ones, has
-// left what the segments start from in the workspace.
+// One walk, into `out`; with heads that share the output, into `part` first.  `states_ready`: what the segments start from is in the workspace.
 tcuscan_status_t walk(WalkArgs W, Heads out, float *part, int dt, hipStream_t s, bool states_ready = false)
 {
     const size_t esz = elem_bytes(dt);
-    const unsigned tiles = W.E <= 64 || W.A > 128 ? 1 : 2, cols = 64 * tiles;           // (256 rows of a state and 32 columns do not fit the registers)
-    const size_t groups = (size_t)W.pieces * W.heads * ((W.E + cols - 1) / cols);
-    const size_t join_groups = (size_t)W.rows * W.heads * (((size_t)W.A * W.E + kJoinThreads - 1) / kJoinThreads);
+    const StateShape shape = state_shape(W.A, W.E);
+    const size_t groups = (size_t)W.pieces * W.heads * ((W.E + shape.columns() - 1) / shape.columns());
+    const size_t join_groups = (size_t)W.rows * W.heads * (shape.floats(W.E) / 4 / kJoinThreads);
     if (groups > kMostBlocks || join_groups > kMostBlocks) return TCUSCAN_ERR_UNSUPPORTED;
     const bool shared = out.heads < W.heads;
     const Heads to = shared ? Heads{part, (long long)W.heads * W.E, W.E, W.heads} : out;
     W.wide = shared;
     const bool new_whole = whole(W.y, W.A, esz) && whole(W.z, W.E, esz), all_whole = new_whole && whole(W.x, W.A, esz) && whole(to, W.E, shared ? 4 : esz) && to.token > 0;
     if (W.segment_log2 != kWholeRows && !states_ready) {
-        if (!launch(walk_for<false>(dt, W.A, new_whole, tiles), groups, 64 * kWalkWaves, &W, s) || !launch((const void *)join_kernel, join_groups, kJoinThreads, &W, s))
+        if (!launch(walk_for<false>(dt, W.A, new_whole, shape.CT), groups, 64 * kWalkWaves, &W, s) || !launch((const void *)join_kernel, join_groups, kJoinThreads, &W, s))
             return TCUSCAN_ERR_HIP;
     }
     W.out = to;
-    if (!launch(walk_for<true>(dt, W.A, all_whole, tiles), groups, 64 * kWalkWaves, &W, s)) return TCUSCAN_ERR_HIP;
+    if (!launch(walk_for<true>(dt, W.A, all_whole, shape.CT), groups, 64 * kWalkWaves, &W, s)) return TCUSCAN_ERR_HIP;
     const size_t items = (size_t)W.total * out.heads * W.E;
     if (!shared || !items) return TCUSCAN_OK;
     SumArgs S = {part, out, W.total, W.heads, W.E};
@@ -962,7 +1020,7 @@ tcuscan_status_t tcuscan_decay_attention(const tcuscan_attention_shape_t *shape,
     W.log_decay = d_log_decay; W.offsets = d_offsets; W.slots = d_slots; W.m_in = d_state_in; W.m_out = d_state_out; W.ws = d_ws;
     W.between = (float *)((char *)d_ws + L.between); W.segment_log2 = L.segment_log2; W.pieces = (unsigned)pieces_for(p, L.segment_log2);
     W.states = (long long)states; W.total = p.total; W.rows = (unsigned)p.rows; W.heads = (unsigned)p.heads;
-    W.A = (unsigned)p.dk; W.E = (unsigned)p.dv; W.m_a = W.between_a = W.E; W.m_e = W.between_e = 1;
+    W.A = (unsigned)p.dk; W.E = (unsigned)p.dv; W.m_a = W.E; W.m_e = 1;
     W.by_new = 1.0f; W.by_read = scale; W.from_end = 0;
     return walk(W, heads_of(d_out, p.o_token, p.o_head, p.heads), nullptr, dt, (hipStream_t)stream);
 }
@@ -1004,18 +1062,19 @@ tcuscan_status_t tcuscan_decay_attention_backward(const tcuscan_attention_shape_
     const unsigned dk = (unsigned)p.dk, dv = (unsigned)p.dv;
     // dq, with the states of the forward pass: S^T
     W.x = o; W.y = v; W.z = k; W.A = dv; W.E = dk; W.m_a = 1; W.m_e = dv; W.m_in = d_state_in;
-    W.between_a = dk; W.between_e = 1;
     W.by_new = 1.0f; W.by_read = scale; W.from_end = 0;
     tcuscan_status_t r = walk(W, heads_of(d_q_grad, p.dq_token, p.dq_head, p.q_heads), part, dt, s);
     if (r != TCUSCAN_OK) return r;
     // dv and the gradient by the first states, from the end: R
     W.by_new = scale; W.by_read = 1.0f; W.from_end = 1; W.m_in = d_state_out_grad; W.m_out = d_state_in_grad;
-    W.x = k; W.y = q; W.z = o; W.A = dk; W.E = dv; W.m_a = W.between_a = dv; W.m_e = W.between_e = 1;
+    W.x = k; W.y = q; W.z = o; W.A = dk; W.E = dv; W.m_a = dv; W.m_e = 1;
+    W.between_turned = L.segment_log2 != kWholeRows ? (float *)((char *)d_ws + L.turned) : nullptr;
     r = walk(W, heads_of(d_v_grad, p.dv_token, p.dv_head, p.v_heads), part, dt, s);
     if (r != TCUSCAN_OK) return r;
     // dk, with the same states, transposed: R^T.  What its segments start from is there.
     W.m_out = nullptr;
-    W.x = v; W.y = o; W.z = q; W.A = dv; W.E = dk; W.m_a = W.between_a = 1; W.m_e = W.between_e = dv;
+    W.between = W.between_turned;
+    W.x = v; W.y = o; W.z = q; W.A = dv; W.E = dk; W.m_a = 1; W.m_e = dv;
     return walk(W, heads_of(d_k_grad, p.dk_token, p.dk_head, p.k_heads), part, dt, s, true);
 }
 
