@@ -154,8 +154,15 @@ template <int N> __device__ __forceinline__ Parts<N> split(f32x8 x)
     Parts<N> parts;
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-        parts.p[n] = __builtin_convertvector(x, bf16x8);
-        x -= __builtin_convertvector(parts.p[n], f32x8);
+        u32x4 pairs = __builtin_bit_cast(u32x4, __builtin_convertvector(x, bf16x8));
+        asm("" : "+v"(pairs));                     // (or every value is converted a second time on its own, to be subtracted)
+        parts.p[n] = __builtin_bit_cast(bf16x8, pairs);
+        if (n + 1 < N)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                x[2 * k] -= bits<float>(pairs[k] << 16);
+                x[2 * k + 1] -= bits<float>(pairs[k] & 0xFFFF0000u);
+            }
     }
     return parts;
 }
