@@ -117,7 +117,8 @@ __device__ __forceinline__ long long state_of(const long long *slots, unsigned r
 // M += Y^T (wZ).  A wavefront owns 16 CT columns of Z, out and M and all A rows of M, in MFMA accumulators from the first token to the
 // last.  The products are ordered so that operands fall into the lanes that have them: the accumulators of M, two row tiles side by side, are
 // the left operand of M^T X^T as they stand (tile rows are dealt so that a lane's eight values are eight consecutive a), and Z's columns are
-// read transposed once, for Z^T P^T and, weighted, for the update.  Only X, Y, Z (shared by all wavefronts of the workgroup) and P go through LDS.
+// read transposed once, for Z^T P^T and, weighted, for the update.  Only X, Y and Z, which all
+// wavefronts of a workgroup share, go through LDS.
 //
 // Precision.  The matrix unit multiplies bf16 and adds in fp32, so every operand is a sum of bf16 parts: bf16 inputs one, f16 two (exact),
 // fp32 three.  What is rounded on the way:
@@ -197,22 +198,22 @@ template <int COLS> struct Tile {
 // Row operand: lane l of group g receives the eight columns k0 + 8 g .. + 7 of row row0 + l (row0 a multiple of 16, k0 of 32).
 template <int COLS> __device__ __forceinline__ int row_lane(int lane) { return Tile<COLS>::at(lane & 15, 8 * (lane >> 4)); }
 template <int COLS> __device__ __forceinline__ bf16x8 row_operand(const bf16_t *tile, int mine, int row0, int k0) { return *(const bf16x8 *)(tile + row0 * COLS + (mine ^ k0)); }
-// Column operand: lane l of group g receives one column of the eight rows row0 + 8 g .. + 7 (row0 a multiple of 32).  The instruction hands lane l of 16 the
-// l-th column of the four rows whose 16 pieces of four columns the 16 lanes point at: lane s at row s / 4 and piece s % 4, which starts PIECE columns behind the
-// one before.  `first`: the wavefront's first column, a multiple of 32 (of 16, if it is the only one); col0: from there, a multiple of 16 or with PIECE = 8
-// of 32, and there + 4 for the other halves of the pieces' granules.
+// Column operand: lane l of group g receives one column of the eight rows 4 g .. 4 g + 3 and 16 + 4 g .. 16 + 4 g + 3 (the order in which P^T's accumulators
+// hold its rows, two tiles of them above each other).  The instruction hands lane l of 16 the l-th column of the four rows whose 16 pieces of four columns
+// the 16 lanes point at: lane s at row s / 4 and piece s % 4, which starts PIECE columns behind the one before.  `first`: the wavefront's first column, a
+// multiple of 32 (of 16, if it is the only one); col0: from there, a multiple of 16 or with PIECE = 8 of 32, and there + 4 for the other halves of the
+// pieces' granules.
 __device__ __forceinline__ s16x4 read_transposed(const bf16_t *p)
 {
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)p);
 }
-template <int COLS, int PIECE> __device__ __forceinline__ int column_lane(int lane, int first) { return Tile<COLS>::at(8 * (lane >> 4) + ((lane & 15) >> 2), first + PIECE * (lane & 3)); }
-template <int COLS> __device__ __forceinline__ bf16x8 column_operand(const bf16_t *tile, int mine, int row0, int col0)
+template <int COLS, int PIECE> __device__ __forceinline__ int column_lane(int lane, int first) { return Tile<COLS>::at(4 * (lane >> 4) + ((lane & 15) >> 2), first + PIECE * (lane & 3)); }
+template <int COLS> __device__ __forceinline__ bf16x8 column_operand(const bf16_t *tile, int mine, int col0)
 {
-    const bf16_t *p = tile + row0 * COLS + (col0 & 4);
-    const int at = mine ^ (col0 & ~4);             // four rows on, the swizzle differs in its lowest bit
-    const s16x4 a = read_transposed(p + at), b = read_transposed(p + 4 * COLS + (at ^ 8));
-    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    const bf16_t *p = tile + (col0 & 4) + (mine ^ (col0 & ~4));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(read_transposed(p), read_transposed(p + 16 * COLS), 0, 1, 2, 3, 4, 5, 6, 7));
 }
+__device__ __forceinline__ int column_row(int g, int k) { return k < 4 ? 4 * g + k : 12 + 4 * g + k; }       // the k-th of these rows
 // Keeps the compiler from computing what depends on v ahead of a loop: addresses made of a lane's number and constants would take dozens of registers.
 template <class T> __device__ __forceinline__ T here(T v)
 {
@@ -450,14 +451,14 @@ template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bo
     typedef typename Elem<DT>::T T;
     constexpr int N = parts_of(DT), C = kBlock, EB = 16 * kWalkWaves * CT, kThreads = 64 * kWalkWaves;
     constexpr bool kDirectly = way_of(DT, WHOLE) == kDirect;
-    constexpr int kTiles = C / 16, kOrder = N == 3 ? 3 : 2;    // tiles of 16 tokens
+    constexpr int kTiles = 2, kOrder = N == 3 ? 3 : 2;         // tiles of 16 tokens
     typedef Stage<DT, C, AP, kThreads, WHOLE> StageA;
     typedef Stage<DT, C, EB, kThreads, WHOLE> StageE;
     // Loads that write LDS themselves go round kRing tiles of each array: while a block is worked on, the kRing - 1 behind it are on their way.
     constexpr int kRing = !kDirectly ? 1 : READS ? 3 : 4, kLoads = (READS ? 2 : 1) * StageA::kSure + StageE::kSure;
     // (Each tile is an array of its own: the compiler has a wavefront wait for loads into an array before it reads from it.)
     constexpr int kX = READS ? N * C * AP : 8, kY = N * C * AP, kZ = N * C * EB, kNone = 8;
-    __shared__ __attribute__((aligned(16))) bf16_t sx0[kX], sx1[kRing > 1 ? kX : kNone], sx2[kRing > 2 ? kX : kNone], sp[READS ? N * C * C : kNone];
+    __shared__ __attribute__((aligned(16))) bf16_t sx0[kX], sx1[kRing > 1 ? kX : kNone], sx2[kRing > 2 ? kX : kNone];
     __shared__ __attribute__((aligned(16))) bf16_t sy0[kY], sy1[kRing > 1 ? kY : kNone], sy2[kRing > 2 ? kY : kNone], sy3[kRing > 3 ? kY : kNone];
     __shared__ __attribute__((aligned(16))) bf16_t sz0[kZ], sz1[kRing > 1 ? kZ : kNone], sz2[kRing > 2 ? kZ : kNone], sz3[kRing > 3 ? kZ : kNone];
 
@@ -495,9 +496,14 @@ template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bo
     const float by_key = W.by_read * W.by_new;
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) reading[t] = W.by_read * decay_power(log_decay, (float)(16 * t + l + (W.from_end ? 0 : 1)));
-    if (READS)                                     // P above its diagonal of tiles: zeros for good
-        for (int i = threadIdx.x; i < N * 32; i += kThreads)
-            *(u32x4 *)(sp + i / 32 * C * C + Tile<C>::at(i / 2 % 16, 16 + 8 * (i % 2))) = u32x4{0u, 0u, 0u, 0u};
+    // and of P^T's rows j = 4 g + r and columns i = l: tiles on the diagonal (nothing where j is behind i) and below it
+    f32x4 on_diagonal, below_diagonal;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int apart = l - 4 * g - r;
+        on_diagonal[r] = apart >= 0 ? by_key * decay_power(log_decay, (float)apart) : 0.0f;
+        below_diagonal[r] = by_key * decay_power(log_decay, (float)(apart + 16));
+    }
 
     const long long sign = W.from_end ? -1 : 1, origin = (W.from_end ? piece.hi - 1 : piece.lo) + sign * piece.first;
     StageA next_x, next_y;
@@ -517,12 +523,12 @@ template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bo
     const bool exact = W.m_out && slot >= 0 && decay_power(log_decay, (float)(piece.hi - piece.lo - piece.end)) > 0.125f;
     const long long length = piece.end - piece.first;
     auto tokens = [&](long long left) { return (int)(left < C ? left : C); };
-    // by_new a^(n-1-j), from the end a^(n-j), of the lane's tokens j = 8 g + k: in whole blocks a power for the lane's group times one for k, which is the
-    // same for all lanes
-    const float group_power = W.by_new * decay_power(log_decay, (float)(C - 8 - 8 * g + (W.from_end ? 1 : 0)));
+    // by_new a^(n-1-j), from the end a^(n-j), of the lane's tokens j = column_row(g, k): in whole blocks a power for the lane's group times one for k, which is
+    // the same for all lanes
+    const float group_power = W.by_new * decay_power(log_decay, (float)(12 - 4 * g + (W.from_end ? 1 : 0)));
     float near_power[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) near_power[k] = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, decay_power(log_decay, (float)(7 - k)))));
+    for (int k = 0; k < 8; ++k) near_power[k] = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, decay_power(log_decay, (float)(19 - column_row(0, k))))));
     auto weights = [&](int n) {
         f32x8 w;
         if (n == C) {
@@ -532,7 +538,7 @@ template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bo
         } else {
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const int j = here(8 * g) + k;
+                const int j = column_row(here(g), k);
                 w[k] = j < n ? W.by_new * decay_power(log_decay, (float)(n - 1 - j + (W.from_end ? 1 : 0))) : 0.0f;
             }
         }
@@ -556,7 +562,7 @@ template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bo
     auto take_block = [&](bf16_t *x_now, bf16_t *x_free, bf16_t *y_now, bf16_t *y_free, bf16_t *z_now, bf16_t *z_free) __attribute__((always_inline)) {
         const long long behind = length - at - C;
         const int n = tokens(length - at);
-        const int row_at = here(row_lane<AP>(lane)), p_at = here(row_lane<C>(lane)), y_at = here(column_lane<AP, 8>(lane, 0)), z_at = here(column_lane<EB, 4 * CT>(lane, wave_e));
+        const int row_at = here(row_lane<AP>(lane)), y_at = here(column_lane<AP, 8>(lane, 0)), z_at = here(column_lane<EB, 4 * CT>(lane, wave_e));
         if constexpr (kDirectly) {
             // of the loads behind this block's, as many may be on their way as there surely are (stores are waited for with them)
             if (kRing > 3 && behind > C) __builtin_amdgcn_s_waitcnt(loads_left((kRing > 3 ? 2 : 1) * kLoads));
@@ -570,51 +576,27 @@ template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bo
         }
         __syncthreads();
         if constexpr (kDirectly) load(x_free, y_free, z_free);
-        if constexpr (READS) {
-            // P^T, 16 keys by 16 queries at a time: three of the wavefronts have a tile on or below the diagonal
-            if (wave < 3) {
-                const int it = wave > 0, jt = wave > 1;
-                f32x4 p = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int s = 0; s < AP / 32; ++s) {
-                    Parts<N> keys, queries;
-#pragma unroll
-                    for (int m = 0; m < N; ++m) {
-                        keys.p[m] = row_operand<AP>(y_now + m * C * AP, row_at, 16 * jt, 32 * s);
-                        queries.p[m] = row_operand<AP>(x_now + m * C * AP, row_at, 16 * it, 32 * s);
-                    }
-                    products<kOrder>([&](int i, int j) { p = mfma(keys.p[i], queries.p[j], p); }, keys, queries);
-                }
-                const int i = 16 * it + l, j = 16 * jt + 4 * g, apart = here(i - j);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) p[r] = apart >= r ? p[r] * (by_key * decay_power(log_decay, (float)(apart - r))) : 0.0f;
-#pragma unroll
-                for (int m = 0; m < N; ++m) {
-                    const bf16x4 part = __builtin_convertvector(p, bf16x4);
-                    *(bf16x4 *)(sp + m * C * C + Tile<C>::at(i, j)) = part;
-                    p -= __builtin_convertvector(part, f32x4);
-                }
-            }
-            __syncthreads();
-        }
         Parts<N> zt[CT];                           // 16 columns of Z by 32 tokens
 #pragma unroll
         for (int c = 0; c < CT; ++c)
 #pragma unroll
-            for (int m = 0; m < N; ++m) zt[c].p[m] = column_operand<EB>(z_now + m * C * EB, z_at, 0, 4 * c);
+            for (int m = 0; m < N; ++m) zt[c].p[m] = column_operand<EB>(z_now + m * C * EB, z_at, 4 * c);
         // what is added to the state
         const f32x8 w = weights(n);
         auto weighted = [&](int c) {
+#pragma clang fp contract(off)                     // (a product rounded once: fused with what a split subtracts, its parts would differ between the two places that split it)
             f32x8 v = __builtin_convertvector(zt[c].p[N - 1], f32x8);
 #pragma unroll
             for (int m = N - 2; m >= 0; --m) v += __builtin_convertvector(zt[c].p[m], f32x8);
             return v * w;
         };
-        constexpr int NM = N == 3 ? 3 : 2;
-        f32x4 o[kTiles][CT];
         if constexpr (READS) {
+            // P^T, by every wavefront for itself (through LDS it would cost a barrier), and M^T X^T, from the same rows of X.  P^T[j][i] of keys' and queries' tile 0 |
+            // of queries' tile 1 with keys' tile 0 and 1
+            constexpr int NM = N == 3 ? 3 : 2;
+            f32x4 o[2][CT], p00 = {}, p01 = {}, p11 = {};
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t)
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int c = 0; c < CT; ++c) o[t][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
             Parts<NM> m[2][CT];                    // this step's parts of M and the next one's
@@ -626,36 +608,42 @@ template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bo
 #pragma unroll
             for (int s = 0; s < AP / 32; ++s) {
                 __builtin_amdgcn_sched_barrier(0);             // (or the parts of all steps take registers at once)
-                Parts<N> b[kTiles];
+                Parts<N> queries[2], keys[2];
 #pragma unroll
-                for (int t = 0; t < kTiles; ++t)
+                for (int t = 0; t < 2; ++t)
 #pragma unroll
-                    for (int i = 0; i < N; ++i) b[t].p[i] = row_operand<AP>(x_now + i * C * AP, row_at, 16 * t, 32 * s);
+                    for (int i = 0; i < N; ++i) {
+                        queries[t].p[i] = row_operand<AP>(x_now + i * C * AP, row_at, 16 * t, 32 * s);
+                        keys[t].p[i] = row_operand<AP>(y_now + i * C * AP, row_at, 16 * t, 32 * s);
+                    }
                 if (s + 1 < AP / 32) split_m(s + 1);
                 products<kOrder>([&](int i, int j) {           // (independent ones behind each other)
+                    p00 = mfma(keys[0].p[i], queries[0].p[j], p00);
+                    p01 = mfma(keys[0].p[i], queries[1].p[j], p01);
+                    p11 = mfma(keys[1].p[i], queries[1].p[j], p11);
+                }, keys[0], queries[0]);
+                products<kOrder>([&](int i, int j) {
 #pragma unroll
                     for (int c = 0; c < CT; ++c)
 #pragma unroll
-                        for (int t = 0; t < kTiles; ++t) o[t][c] = mfma(m[s & 1][c].p[i], b[t].p[j], o[t][c]);
-                }, m[0][0], b[0]);
+                        for (int t = 0; t < 2; ++t) o[t][c] = mfma(m[s & 1][c].p[i], queries[t].p[j], o[t][c]);
+                }, m[0][0], queries[0]);
             }
-        }
-        if constexpr (READS) {
+            p00 *= on_diagonal;
+            p01 *= below_diagonal;
+            p11 *= on_diagonal;
+            const f32x4 none = {0.0f, 0.0f, 0.0f, 0.0f};
+            const Parts<N> p[2] = {split<N>(__builtin_shufflevector(p00, none, 0, 1, 2, 3, 4, 5, 6, 7)), split<N>(__builtin_shufflevector(p01, p11, 0, 1, 2, 3, 4, 5, 6, 7))};
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t)
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int c = 0; c < CT; ++c) o[t][c] *= reading[t];
-            Parts<N> b[kTiles];
-#pragma unroll
-            for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-                for (int i = 0; i < N; ++i) b[t].p[i] = row_operand<C>(sp + i * C * C, p_at, 16 * t, 0);
             products<kOrder>([&](int i, int j) {
 #pragma unroll
-                for (int t = 0; t < kTiles; ++t)
+                for (int t = 0; t < 2; ++t)
 #pragma unroll
-                    for (int c = 0; c < CT; ++c) o[t][c] = mfma(zt[c].p[i], b[t].p[j], o[t][c]);
-            }, zt[0], b[0]);
+                    for (int c = 0; c < CT; ++c) o[t][c] = mfma(zt[c].p[i], p[t].p[j], o[t][c]);
+            }, zt[0], p[0]);
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) {
                 if (16 * t + l >= n) continue;
@@ -676,7 +664,7 @@ template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bo
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int m = 0; m < N; ++m) yt[t / 2 & 1][u].p[m] = column_operand<AP>(y_now + m * C * AP, y_at, 0, 16 * t + 4 * u);
+                for (int m = 0; m < N; ++m) yt[t / 2 & 1][u].p[m] = column_operand<AP>(y_now + m * C * AP, y_at, 16 * t + 4 * u);
         };
         load_y(0);
 #pragma unroll
@@ -702,7 +690,7 @@ template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bo
                 for (int t = 0; t < AP / 16; ++t)
 #pragma unroll
                     for (int m = 0; m < N; ++m) {
-                        const bf16x8 y_part = column_operand<AP>(y_now + m * C * AP, y_at, 0, 32 * (t / 2) + 4 * (t & 1));
+                        const bf16x8 y_part = column_operand<AP>(y_now + m * C * AP, y_at, 32 * (t / 2) + 4 * (t & 1));
 #pragma unroll
                         for (int c = 0; c < CT; ++c) M[t][c] = mfma(y_part, third[c].p[2 - m], M[t][c]);
                     }
