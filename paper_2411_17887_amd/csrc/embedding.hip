@@ -13,6 +13,7 @@
 #include "../../include/tcuscan.h"
 #include "chain_layout.h"
 #include "element_types.h"
+#include "wave_ops.h"
 
 namespace {
 
@@ -130,66 +131,104 @@ __global__ __launch_bounds__(kThreads) void token_keys_kernel(GradArgs A)
     A.tokens[t] = (uint32_t)t;
 }
 
-// Few tokens: no sort.  A workgroup takes `rows` rows of the table, looks all token numbers over and keeps those of its rows in order; a
-// wavefront then sums a row at a time.  One launch.
-constexpr int kFewTokens = 4096, kMaxFewRows = 64;
+// Few tokens: no sort.  A workgroup takes `rows` rows of the table and a slice of the columns.  Each of its wavefronts looks a quarter of the token numbers over
+// and lists those of its rows in order, then sums them row by row; a row that several quarters have is put together in LDS, in the order of the
+// quarters.  One launch, whose time is that of its dependent steps: the numbers, a gradient's rows eight at a time, the table's row.
+constexpr int kFewTokens = 4096, kMaxFewRows = 64, kWaves = kThreads / 64, kQuarter = kFewTokens / kWaves;
 template <int DG, int DW, bool ALIGNED> __global__ __launch_bounds__(kThreads) void few_tokens_kernel(GradArgs A)
 {
     typedef Lane<DG, ALIGNED> L;
     typedef typename L::G G;
-    constexpr int kWaves = kThreads / 64;
-    __shared__ uint32_t list[kFewTokens];          // (row of the workgroup) << 16 | token, in the order of the tokens
-    __shared__ int counts[kWaves];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const size_t first = (size_t)blockIdx.x * A.rows;
-    int listed = 0;
-    for (size_t t0 = 0; t0 < A.n; t0 += kThreads) {
-        const size_t t = t0 + threadIdx.x;
-        const long long id = t < A.n ? id_at(A.ids, A.wide_ids, t) : -1;
-        if (blockIdx.x == 0 && id >= (long long)A.vocab) raise_fault(A.ws, kFaultBadIndex);
-        const bool mine = id >= (long long)first && id < (long long)(first + A.rows) && id < (long long)A.vocab && id != A.padding;
-        const uint64_t votes = __ballot(mine);
-        if (lane == 0) counts[wave] = __popcll(votes);
-        __syncthreads();
-        int at = listed, all = 0;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            if (w < wave) at += counts[w];
-            all += counts[w];
-        }
-        if (mine) list[at + __popcll(votes & (((uint64_t)1 << lane) - 1))] = (uint32_t)(id - (long long)first) << 16 | (uint32_t)t;
-        listed += all;
-        __syncthreads();
-    }
+    typedef typename Elem<DW>::T W;
+    __shared__ uint32_t list[kWaves][kQuarter];    // (row of the workgroup) << 16 | token
+    __shared__ uint64_t rows_of[kWaves];           // rows that a quarter has
+    __shared__ float part[2][kWaves][L::N * 64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const size_t first = blockIdx.x / A.slices * A.rows, c0 = blockIdx.x % A.slices * L::kSlice;
     const size_t last = first + A.rows < A.vocab ? first + A.rows : A.vocab;
-    for (size_t row = first + wave; row < last; row += kWaves) {
-        typename Elem<DW>::T *w = (typename Elem<DW>::T *)A.d_weight + row * A.weight_stride;
-        bool any = false;
-        for (size_t c0 = 0; c0 < A.dim; c0 += L::kSlice) {
-            float sum[L::N] = {};
-            for (int i0 = 0; i0 < listed; i0 += 64) {
-                const uint32_t item = i0 + lane < listed ? list[i0 + lane] : 0xFFFFFFFFu;
-                uint64_t votes = __ballot(item >> 16 == (uint32_t)(row - first));
-                any |= votes != 0;
-                while (votes) {                    // four rows of gradients on their way at a time
-                    const G *from[4];
-                    typename L::Vec v[4];
-                    int k = 0;
+    int listed = 0;
+    uint64_t mine = 0;
+    {
+        const size_t quarter = ((A.n + kWaves - 1) / kWaves + 63) & ~(size_t)63, begin = wave * quarter, end = begin + quarter < A.n ? begin + quarter : A.n;
+        constexpr int kAhead = 8;
+        for (size_t t0 = begin; t0 < end; t0 += 64 * kAhead) {
+            long long id[kAhead];
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        const int source = votes ? __builtin_ctzll(votes) : -1;
-                        if (source >= 0) { votes &= votes - 1; k = u + 1; }
-                        from[u] = (const G *)A.d_out + (size_t)(__builtin_amdgcn_readlane((int)item, source < 0 ? 0 : source) & 0xFFFF) * A.out_stride;
-                    }
-#pragma unroll
-                    for (int u = 0; u < 4; ++u)
-                        if (u < k) v[u] = L::load(from[u], c0, A.dim, lane);
-#pragma unroll
-                    for (int u = 0; u < 4; ++u)
-                        if (u < k) L::add(sum, v[u]);
-                }
+            for (int u = 0; u < kAhead; ++u) {
+                const size_t t = t0 + 64 * u + lane;
+                id[u] = t < end ? id_at(A.ids, A.wide_ids, t) : -1;
             }
-            if (any || !A.accumulate) L::template finish<DW>(w, c0, A.dim, lane, sum, A.scale, A.accumulate);
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                if (blockIdx.x == 0 && id[u] >= (long long)A.vocab) raise_fault(A.ws, kFaultBadIndex);
+                const bool in = id[u] >= (long long)first && id[u] < (long long)last && id[u] != A.padding;
+                const uint64_t votes = __ballot(in);
+                if (!votes) continue;
+                const uint32_t row = (uint32_t)(id[u] - (long long)first);
+                if (in) {
+                    list[wave][listed + __popcll(votes & (((uint64_t)1 << lane) - 1))] = row << 16 | (uint32_t)(t0 + 64 * u + lane);
+                    mine |= (uint64_t)1 << row;
+                }
+                listed += __popcll(votes);
+            }
+        }
+    }
+    const uint64_t has = (uint64_t)wave_or((uint32_t)(mine >> 32)) << 32 | wave_or((uint32_t)mine);
+    if (lane == 0) rows_of[wave] = has;
+    __syncthreads();
+    uint64_t any = 0, several = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        several |= any & rows_of[w];
+        any |= rows_of[w];
+    }
+    W *const table = (W *)A.d_weight + first * A.weight_stride;
+    auto sum_row = [&](int row, float (&sum)[L::N]) {          // of the wavefront's own list
+        for (int i0 = 0; i0 < listed; i0 += 64) {
+            const uint32_t item = i0 + lane < listed ? list[wave][i0 + lane] : 0xFFFFFFFFu;
+            uint64_t votes = __ballot(item >> 16 == (uint32_t)row);
+            while (votes) {
+                constexpr int kAhead = 8;
+                typename L::Vec v[kAhead];
+                int count = 0;
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u) {
+                    if (!votes) break;
+                    const int source = __builtin_ctzll(votes);
+                    votes &= votes - 1;
+                    count = u + 1;
+                    v[u] = L::load((const G *)A.d_out + (size_t)(__builtin_amdgcn_readlane((int)item, source) & 0xFFFF) * A.out_stride, c0, A.dim, lane);
+                }
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u)
+                    if (u < count) L::add(sum, v[u]);
+            }
+        }
+    };
+    const int rows = (int)(last - first);
+    for (int row = 0; row < rows; ++row) {         // rows of one quarter, and of none
+        const bool own = has >> row & 1 && !(several >> row & 1), empty = !(any >> row & 1) && row % kWaves == wave && !A.accumulate;
+        if (!own && !empty) continue;
+        float sum[L::N] = {};
+        if (own) sum_row(row, sum);
+        L::template finish<DW>(table + (size_t)row * A.weight_stride, c0, A.dim, lane, sum, A.scale, A.accumulate);
+    }
+    int turn = 0;
+    for (uint64_t left = several; left; left &= left - 1, turn ^= 1) {
+        const int row = __builtin_ctzll(left);
+        float sum[L::N] = {};
+        if (has >> row & 1) sum_row(row, sum);
+#pragma unroll
+        for (int k = 0; k < L::N; ++k) part[turn][wave][k * 64 + lane] = sum[k];
+        __syncthreads();                           // (the other half is free for the next row: its readers have passed the barrier before)
+        if (row % kWaves == wave) {
+#pragma unroll
+            for (int k = 0; k < L::N; ++k) {
+                sum[k] = part[turn][0][k * 64 + lane];
+#pragma unroll
+                for (int w = 1; w < kWaves; ++w) sum[k] += part[turn][w][k * 64 + lane];
+            }
+            L::template finish<DW>(table + (size_t)row * A.weight_stride, c0, A.dim, lane, sum, A.scale, A.accumulate);
         }
     }
 }
@@ -270,19 +309,21 @@ template <int DG, int DW, bool ALIGNED> __global__ __launch_bounds__(kThreads) v
     }
 }
 
-// The runs that lie in several pieces.  A workgroup looks at one piece and a slice of 64 columns: if a run starts in it and goes on behind it, its wavefronts
+// The runs that lie in several pieces.  A workgroup looks at one piece and a slice of 64 VEC columns: if a run starts in it and goes on behind it, its wavefronts
 // take the pieces that hold it in turns of consecutive ones, and the first of them adds the others' sums.
 constexpr int kJoinWaves = 8;
-template <int DW> __global__ __launch_bounds__(64 * kJoinWaves) void join_runs_kernel(GradArgs A)
+template <int DW, int VEC> __global__ __launch_bounds__(64 * kJoinWaves) void join_runs_kernel(GradArgs A)
 {
     typedef typename Elem<DW>::T W;
-    const size_t piece = blockIdx.x, behind = (piece + 1) * A.piece;
+    typedef float Vec __attribute__((ext_vector_type(VEC)));
+    typedef W WVec __attribute__((ext_vector_type(VEC)));
+    const size_t slices = (A.dim + 64 * VEC - 1) / (64 * VEC), piece = blockIdx.x / slices, behind = (piece + 1) * A.piece;
     if (behind >= A.n) return;
     const uint32_t row = A.keys[behind];
     if (A.keys[behind - 1] != row || row >= A.vocab) return;
     if (piece > 0 && A.keys[piece * A.piece] == row && A.keys[piece * A.piece - 1] == row) return;      // (the run started before)
     __shared__ size_t end;
-    __shared__ float sums[kJoinWaves][64];
+    __shared__ Vec sums[kJoinWaves][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if (threadIdx.x == 0) {
         size_t lo = behind, hi = A.n;              // the first pair behind the run
@@ -294,22 +335,31 @@ template <int DW> __global__ __launch_bounds__(64 * kJoinWaves) void join_runs_k
     }
     __syncthreads();
     const size_t count = end - piece, each = (count + kJoinWaves - 1) / kJoinWaves;
-    const size_t from = piece + wave * each, to = from + each < end ? from + each : end;
-    for (size_t c0 = 0; c0 < A.dim; c0 += 64) {
-        const size_t c = c0 + lane;
-        float sum = 0.0f;
-        if (c < A.dim)
-            for (size_t p = from; p < to; ++p) sum += A.partial[(2 * p + (p == piece ? 1 : 0)) * A.dim + c];
-        sums[wave][lane] = sum;
-        __syncthreads();
-        if (wave == 0 && c < A.dim) {
+    const size_t from = piece + wave * each, to = from + each < end ? from + each : end, c = (blockIdx.x % slices * 64 + lane) * VEC;
+    Vec sum = {};
+    if (c < A.dim) {
+        constexpr size_t kAhead = 8;
+        for (size_t p = from; p < to; p += kAhead) {
+            Vec v[kAhead];
 #pragma unroll
-            for (int w = 1; w < kJoinWaves; ++w) sum += sums[w][lane];
-            W *to_row = (W *)A.d_weight + (size_t)row * A.weight_stride;
-            to_row[c] = (W)(A.accumulate ? fmaf(sum, A.scale, (float)to_row[c]) : sum * A.scale);
+            for (size_t u = 0; u < kAhead; ++u) {
+                v[u] = Vec{};
+                if (p + u < to) v[u] = *(const Vec *)(A.partial + (2 * (p + u) + (p + u == piece ? 1 : 0)) * A.dim + c);
+            }
+#pragma unroll
+            for (size_t u = 0; u < kAhead; ++u) sum += v[u];
         }
-        __syncthreads();
     }
+    sums[wave][lane] = sum;
+    __syncthreads();
+    if (wave != 0 || c >= A.dim) return;
+#pragma unroll
+    for (int w = 1; w < kJoinWaves; ++w) sum += sums[w][lane];
+    WVec *to_row = (WVec *)((W *)A.d_weight + (size_t)row * A.weight_stride + c), x;
+    const WVec old = A.accumulate ? *to_row : WVec{};
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) x[k] = (W)(A.accumulate ? fmaf(sum[k], A.scale, (float)old[k]) : sum[k] * A.scale);
+    *to_row = x;
 }
 
 // A kernel for two element types (checked before).
@@ -349,7 +399,7 @@ struct GradLayout {
         tokens_tmp = tokens + words;
         positions = tokens_tmp + words;
         flags = positions + words;
-        partial = flags + (n + 15) / 16 * 16;
+        partial = (flags + n + 255) / 256 * 256;
         all = partial + 2 * ((n + piece_for(n) - 1) / piece_for(n)) * dim * 4;
     }
 };
@@ -415,10 +465,13 @@ tcuscan_status_t tcuscan_embedding_backward(const void *d_ids, int id_bytes, siz
     const bool aligned = dim % cols == 0 && out_stride % cols == 0 && weight_stride % cols == 0 && (uintptr_t)d_out_grad % 16 == 0 && (uintptr_t)d_weight_grad % (cols * we) == 0;
     if (n <= kFewTokens) {
         // as many workgroups as keep the chip busy, and no more than that: each of them reads all token numbers
+        A.slices = (dim + 64 * cols - 1) / (64 * cols);
         A.rows = 4;
-        while (A.rows < kMaxFewRows && vocab / A.rows > 1024) A.rows *= 2;
+        while (A.rows < kMaxFewRows && (vocab + A.rows - 1) / A.rows * A.slices > 2048) A.rows *= 2;
+        const size_t groups = (vocab + A.rows - 1) / A.rows * A.slices;
+        if (groups > kMostRows) return TCUSCAN_ERR_UNSUPPORTED;
         const void *fn = aligned ? pick<FewAligned>(out_dt, weight_dt) : pick<Few>(out_dt, weight_dt);
-        return hipLaunchKernel(fn, dim3((unsigned)((vocab + A.rows - 1) / A.rows)), dim3(kThreads), args, 0, s) == hipSuccess ? TCUSCAN_OK : TCUSCAN_ERR_HIP;
+        return hipLaunchKernel(fn, dim3((unsigned)groups), dim3(kThreads), args, 0, s) == hipSuccess ? TCUSCAN_OK : TCUSCAN_ERR_HIP;
     }
     if (hipLaunchKernel((const void *)token_keys_kernel, dim3((unsigned)((n + kThreads - 1) / kThreads)), dim3(kThreads), args, 0, s) != hipSuccess) return TCUSCAN_ERR_HIP;
     int bits = 0;
@@ -433,8 +486,12 @@ tcuscan_status_t tcuscan_embedding_backward(const void *d_ids, int id_bytes, siz
     if (A.piece_groups + zero_groups > kMostRows) return TCUSCAN_ERR_UNSUPPORTED;
     const void *fn = aligned ? pick<RunsAligned>(out_dt, weight_dt) : pick<Runs>(out_dt, weight_dt);
     if (hipLaunchKernel(fn, dim3((unsigned)(A.piece_groups + zero_groups)), dim3(kThreads), args, 0, s) != hipSuccess) return TCUSCAN_ERR_HIP;
-    fn = weight_dt == kF16 ? (const void *)join_runs_kernel<kF16> : weight_dt == kF32 ? (const void *)join_runs_kernel<kF32> : (const void *)join_runs_kernel<kBF16>;
-    return hipLaunchKernel(fn, dim3((unsigned)pieces), dim3(64 * kJoinWaves), args, 0, s) == hipSuccess ? TCUSCAN_OK : TCUSCAN_ERR_HIP;
+    const size_t by = aligned ? 4 : 1, join_groups = pieces * ((dim + 64 * by - 1) / (64 * by));
+    if (join_groups > kMostRows) return TCUSCAN_ERR_UNSUPPORTED;
+    fn = weight_dt == kF16 ? aligned ? (const void *)join_runs_kernel<kF16, 4> : (const void *)join_runs_kernel<kF16, 1>
+       : weight_dt == kF32 ? aligned ? (const void *)join_runs_kernel<kF32, 4> : (const void *)join_runs_kernel<kF32, 1>
+                           : aligned ? (const void *)join_runs_kernel<kBF16, 4> : (const void *)join_runs_kernel<kBF16, 1>;
+    return hipLaunchKernel(fn, dim3((unsigned)join_groups), dim3(64 * kJoinWaves), args, 0, s) == hipSuccess ? TCUSCAN_OK : TCUSCAN_ERR_HIP;
 }
 
 }  // extern "C"
