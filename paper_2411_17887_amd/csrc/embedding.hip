@@ -32,21 +32,30 @@ __device__ __forceinline__ long long id_at(const void *ids, int wide, size_t i)
     return wide ? ((const long long *)ids)[i] : (long long)((const int *)ids)[i];
 }
 
-// Columns of a row that one lane holds: a wavefront takes 64 * kLaneCols of them at a time.  ALIGNED: a lane's columns are next to each other and
-// load as whole granules; otherwise they are 64 apart, so that rows of any length and start load in runs of 64 elements.
+// Columns of a row that one lane holds: a wavefront takes 64 * kLaneCols of them at a time.  ALIGNED: columns next to each other load and store as whole
+// granules, eight of 16-bit types; where one of two types is fp32, two times four 256 columns apart, so that the fp32 side, too, moves 1 KiB of consecutive
+// bytes an instruction (fp32 rows stored 32 bytes a lane: 45.5 -> 55 us for 65536 bf16 rows of 1024 looked up).  Otherwise a lane's columns are 64 apart,
+// so that rows of any length and start load in runs of 64 elements.
 template <int DG> constexpr int kLaneCols = DG == kF32 ? 4 : 8;
-template <int DG, bool ALIGNED> struct Lane {
+template <int DG, int DOTHER, bool ALIGNED> struct Lane {
     typedef typename Elem<DG>::T G;
-    static constexpr int N = kLaneCols<DG>, kSlice = 64 * N;
+    static constexpr int N = kLaneCols<DG>, kSlice = 64 * N, kGroup = DOTHER == kF32 ? 4 : N;
     template <class X> using VecOf = X __attribute__((ext_vector_type(N)));
+    template <class X> using GroupOf = X __attribute__((ext_vector_type(kGroup)));
     typedef VecOf<G> Vec;
-    static __device__ __forceinline__ size_t col(int lane, int k) { return ALIGNED ? (size_t)lane * N + k : (size_t)k * 64 + lane; }
+    static __device__ __forceinline__ size_t col(int lane, int k) { return ALIGNED ? (size_t)(k / kGroup) * 64 * kGroup + lane * kGroup + k % kGroup : (size_t)k * 64 + lane; }
     // Columns of `row` from c0 on; those from `dim` on are zeros.  (ALIGNED: dim is a multiple of N.)
     template <class X> static __device__ __forceinline__ VecOf<X> load(const X *row, size_t c0, size_t dim, int lane)
     {
         VecOf<X> v{};
         if constexpr (ALIGNED) {
-            if (c0 + (size_t)lane * N < dim) v = *(const VecOf<X> *)(row + c0 + (size_t)lane * N);
+#pragma unroll
+            for (int k = 0; k < N; k += kGroup)
+                if (c0 + col(lane, k) < dim) {
+                    const GroupOf<X> g = *(const GroupOf<X> *)(row + c0 + col(lane, k));
+#pragma unroll
+                    for (int i = 0; i < kGroup; ++i) v[k + i] = g[i];
+                }
         } else {
 #pragma unroll
             for (int k = 0; k < N; ++k) v[k] = c0 + col(lane, k) < dim ? row[c0 + col(lane, k)] : (X)0.0f;
@@ -58,18 +67,21 @@ template <int DG, bool ALIGNED> struct Lane {
 #pragma unroll
         for (int k = 0; k < N; ++k) sum[k] += (float)v[k];
     }
-    // The finished row: scaled, added to what is there or not, rounded.
-    template <int DW> static __device__ __forceinline__ void finish(typename Elem<DW>::T *row, size_t c0, size_t dim, int lane, const float (&sum)[N], float scale, bool accumulate)
+    // The finished row: scaled, added to what is there or not, rounded.  AROUND: past the caches, for what is not read again soon.
+    template <int DW, bool AROUND = false> static __device__ __forceinline__ void finish(typename Elem<DW>::T *row, size_t c0, size_t dim, int lane, const float (&sum)[N], float scale, bool accumulate)
     {
         typedef typename Elem<DW>::T W;
         if constexpr (ALIGNED) {
-            typedef W WVec __attribute__((ext_vector_type(N)));
-            if (c0 + (size_t)lane * N >= dim) return;
-            WVec *p = (WVec *)(row + c0 + (size_t)lane * N), w;
-            const WVec old = accumulate ? *p : WVec{};
 #pragma unroll
-            for (int k = 0; k < N; ++k) w[k] = (W)(accumulate ? fmaf(sum[k], scale, (float)old[k]) : sum[k] * scale);
-            *p = w;
+            for (int k = 0; k < N; k += kGroup) {
+                if (c0 + col(lane, k) >= dim) continue;
+                GroupOf<W> *p = (GroupOf<W> *)(row + c0 + col(lane, k)), w;
+                const GroupOf<W> old = accumulate ? *p : GroupOf<W>{};
+#pragma unroll
+                for (int i = 0; i < kGroup; ++i) w[i] = (W)(accumulate ? fmaf(sum[k + i], scale, (float)old[i]) : sum[k + i] * scale);
+                if constexpr (AROUND) __builtin_nontemporal_store(w, p);
+                else *p = w;
+            }
         } else {
 #pragma unroll
             for (int k = 0; k < N; ++k) {
@@ -84,7 +96,7 @@ template <int DG, bool ALIGNED> struct Lane {
 // over as many wavefronts as there are.)
 template <int DW, int DO, bool ALIGNED, int kTokens> __global__ __launch_bounds__(kThreads) void lookup_kernel(LookupArgs A)
 {
-    typedef Lane<DW == kF32 ? DO : DW, ALIGNED> L;             // (eight columns to a lane unless both types are fp32)
+    typedef Lane<DW == kF32 ? DO : DW, DW == kF32 ? DW : DO, ALIGNED> L;       // (eight columns to a lane unless both types are fp32)
     typedef typename Elem<DW>::T W;
     const int lane = threadIdx.x & 63;
     const size_t item = (size_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6), t0 = item / A.slices * kTokens, c0 = item % A.slices * L::kSlice;
@@ -104,7 +116,7 @@ template <int DW, int DO, bool ALIGNED, int kTokens> __global__ __launch_bounds_
         float f[L::N];
 #pragma unroll
         for (int k = 0; k < L::N; ++k) f[k] = (float)v[u][k];
-        L::template finish<DO>((typename Elem<DO>::T *)A.out + (t0 + u) * A.out_stride, c0, A.dim, lane, f, A.scale, false);
+        L::template finish<DO, (kTokens > 1)>((typename Elem<DO>::T *)A.out + (t0 + u) * A.out_stride, c0, A.dim, lane, f, A.scale, false);
     }
 }
 
@@ -115,7 +127,7 @@ struct GradArgs {
     float *partial;
     size_t n, vocab, dim, out_stride, weight_stride;
     long long padding;
-    size_t piece, slices, piece_groups, rows;      // rows: of the table to a workgroup, where there are few tokens
+    size_t piece, slices, piece_groups, zero_groups, rows;      // rows: of the table to a workgroup, where there are few tokens
     float scale;
     int wide_ids, accumulate;
 };
@@ -137,7 +149,7 @@ __global__ __launch_bounds__(kThreads) void token_keys_kernel(GradArgs A)
 constexpr int kFewTokens = 4096, kMaxFewRows = 64, kWaves = kThreads / 64, kQuarter = kFewTokens / kWaves;
 template <int DG, int DW, bool ALIGNED> __global__ __launch_bounds__(kThreads) void few_tokens_kernel(GradArgs A)
 {
-    typedef Lane<DG, ALIGNED> L;
+    typedef Lane<DG, DW, ALIGNED> L;
     typedef typename L::G G;
     typedef typename Elem<DW>::T W;
     __shared__ uint32_t list[kWaves][kQuarter];    // (row of the workgroup) << 16 | token
@@ -236,17 +248,19 @@ template <int DG, int DW, bool ALIGNED> __global__ __launch_bounds__(kThreads) v
 // Many tokens.  The sorted pairs are cut into pieces of `piece` pairs, whatever runs they hold, so that a frequent token's run is shared by many
 // wavefronts: a wavefront takes a piece and a slice of the columns.  Runs that lie inside a piece are finished there; what a piece has of
 // a run that goes on beyond it is kept, in fp32, in one of the piece's two places (0: the run comes from the piece before, 1: it starts here)
-// and added up, piece by piece in their order, by join_runs_kernel.  Workgroups behind the pieces' write zeros into rows that no token took.
+// and added up, piece by piece in their order, by join_runs_kernel.  Every second workgroup, as long as both are left, writes zeros into rows that no token took.
 constexpr int kMaxPiece = 32, kZeroRows = 64;
 template <int DG, int DW, bool ALIGNED> __global__ __launch_bounds__(kThreads) void sum_runs_kernel(GradArgs A)
 {
-    typedef Lane<DG, ALIGNED> L;
+    typedef Lane<DG, DW, ALIGNED> L;
     typedef typename L::G G;
     typedef typename Elem<DW>::T W;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    if (blockIdx.x >= A.piece_groups) {
+    // pieces and rows to clear take turns, so that reading and writing go side by side
+    const size_t both = A.piece_groups < A.zero_groups ? A.piece_groups : A.zero_groups, index = blockIdx.x < 2 * both ? blockIdx.x / 2 : blockIdx.x - both;
+    if (blockIdx.x < 2 * both ? blockIdx.x & 1 : A.zero_groups > both) {
         __shared__ uint64_t taken;
-        const size_t first = (size_t)(blockIdx.x - A.piece_groups) * kZeroRows;
+        const size_t first = index * kZeroRows;
         if (wave == 0) {
             const uint32_t row = (uint32_t)first + lane;
             size_t lo = 0, hi = A.n;               // the first pair whose key is not below the row
@@ -264,7 +278,7 @@ template <int DG, int DW, bool ALIGNED> __global__ __launch_bounds__(kThreads) v
                 for (size_t c0 = 0; c0 < A.dim; c0 += L::kSlice) L::template finish<DW>((W *)A.d_weight + (first + r) * A.weight_stride, c0, A.dim, lane, zeros, 0.0f, false);
         return;
     }
-    const size_t item = (size_t)blockIdx.x * (kThreads / 64) + wave, piece = item / A.slices, c0 = item % A.slices * L::kSlice;
+    const size_t item = index * (kThreads / 64) + wave, piece = item / A.slices, c0 = item % A.slices * L::kSlice;
     const size_t begin = piece * A.piece;
     if (begin >= A.n) return;
     const int count = (int)(begin + A.piece < A.n ? A.piece : A.n - begin);
@@ -311,7 +325,7 @@ template <int DG, int DW, bool ALIGNED> __global__ __launch_bounds__(kThreads) v
 
 // The runs that lie in several pieces.  A workgroup looks at one piece and a slice of 64 VEC columns: if a run starts in it and goes on behind it, its wavefronts
 // take the pieces that hold it in turns of consecutive ones, and the first of them adds the others' sums.
-constexpr int kJoinWaves = 8;
+constexpr int kJoinWaves = 4;
 template <int DW, int VEC> __global__ __launch_bounds__(64 * kJoinWaves) void join_runs_kernel(GradArgs A)
 {
     typedef typename Elem<DW>::T W;
@@ -482,6 +496,7 @@ tcuscan_status_t tcuscan_embedding_backward(const void *d_ids, int id_bytes, siz
     A.piece = piece_for(n);
     A.slices = (dim + 64 * cols - 1) / (64 * cols);
     const size_t pieces = (n + A.piece - 1) / A.piece, zero_groups = accumulate ? 0 : (vocab + kZeroRows - 1) / kZeroRows;
+    A.zero_groups = zero_groups;
     A.piece_groups = (pieces * A.slices + kThreads / 64 - 1) / (kThreads / 64);
     if (A.piece_groups + zero_groups > kMostRows) return TCUSCAN_ERR_UNSUPPORTED;
     const void *fn = aligned ? pick<RunsAligned>(out_dt, weight_dt) : pick<Runs>(out_dt, weight_dt);
