@@ -297,3 +297,43 @@ def test_offsets_and_slots_out_of_range_are_reported_and_touch_nothing_outside()
     tcuscan.decay_attention_step(*(x[:2] for x in c.qkv), torch.empty(2, 1, 32, dtype=c.dt, device="cuda"), c.log_decay, state[:3], slots=torch.tensor([1, 3]).cuda(), ws=ws)
     torch.cuda.synchronize()
     assert tcuscan.workspace_fault(ws) == 2 and (state[3:] == 0).all() and (state[1] != 0).any()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_long_rows_with_states_in_place(kind):
+    """Rows of several segments that start from and end in the same array: no segment may see the states already written."""
+    import torch
+    c = Case(kind, [900, 0, 1100, 64], heads=(2, 2, 2), dk=64, dv=48, decays=[0.9995, 0.97], seed=17)
+    state, out = c.s0.cuda(), torch.empty(c.total, 2, 48, dtype=c.dt, device="cuda")
+    ws = tcuscan.new_decay_attention_workspace(c.rows, c.total, 2, 64, 48, dt=kind)
+    tcuscan.decay_attention(*c.qkv, out, c.log_decay, c.offs, scale=c.scale, state_in=state, state_out=state, ws=ws)
+    torch.cuda.synchronize()
+    c.check_forward(out, state)
+
+
+@pytest.mark.parametrize("stride", [4_000_000, 5_000_000])
+def test_tokens_further_apart_than_32_bits_reach(stride):
+    """Tokens 4 and 5 million elements apart (within and beyond what offsets of a block take): the last ones lie beyond 2^32 bytes."""
+    import torch
+    c = Case("bf16", [600], heads=(1, 1, 1), dk=32, dv=32, seed=18)
+    far = [torch.empty(stride * 599 + 32, dtype=torch.bfloat16, device="cuda").as_strided((600, 1, 32), (stride, 32, 1)) for _ in range(2)]
+    far[0].copy_(c.qkv[1])
+    c.qkv[1] = far[0]
+    out, state_out = c.forward()
+    c.check_forward(out, state_out)
+    ws = tcuscan.new_decay_attention_workspace(1, 600, 1, 32, 32)
+    tcuscan.decay_attention(*c.qkv, far[1], c.log_decay, c.offs, scale=c.scale, state_in=c.s0.cuda(), state_out=state_out, ws=ws)
+    torch.cuda.synchronize()
+    c.check_forward(far[1].contiguous(), state_out)
+
+
+def test_inputs_shared_by_all_tokens_or_heads_without_copies():
+    """Strides of 0: one key for all tokens, one query for all heads."""
+    import torch
+    c = Case("bf16", [200, 30], heads=(3, 3, 3), dk=32, dv=32, seed=19)
+    k = c.qkv[1][:1].expand(c.total, 3, 32)
+    q = c.qkv[0][:, :1].expand(c.total, 3, 32)
+    c.qkv = [q, k, c.qkv[2]]
+    c.host = [x.double().cpu().numpy() for x in c.qkv]
+    assert k.stride(0) == 0 and q.stride(1) == 0
+    c.check_forward(*c.forward())

@@ -116,10 +116,8 @@ def test_gradient_in_all_types(g_kind, w_kind, accumulate):
 
 
 @pytest.mark.parametrize("dim", [1, 3, 8, 65, 515, 1024, 4100])
-@pytest.mark.parametrize("n,vocab", [(0, 7), (1, 1), (1, 900), (70, 3), (700, 2000), (9001, 50)])
+@pytest.mark.parametrize("n,vocab", [(0, 7), (1, 1), (1, 900), (70, 3), (700, 2000), (4097, 50)])
 def test_gradient_of_all_sizes(n, vocab, dim):
-    if n * dim > 10_000_000:
-        pytest.skip("the definition in 64 bits would take too long")
     for pad in (0, 1):
         check_gradient(zipf(n, vocab, 6), vocab, dim, "bf16", "f32", pad=pad, accumulate=pad == 1, id_type=np.int32 if pad else np.int64)
 
@@ -203,3 +201,30 @@ def test_gradient_in_a_graph():
         tcuscan.embedding_backward(ids, d_out, eager, ws=other)
         torch.cuda.synchronize()
         assert torch.equal(d_weight, eager)
+
+
+def test_rows_further_apart_than_32_bits_reach():
+    """A table and a gradient of more than 2^32 bytes."""
+    import torch
+    vocab, dim = 1_100_000, 2048
+    weight = torch.empty(vocab, dim, dtype=torch.bfloat16, device="cuda")
+    ids = torch.tensor([0, vocab - 1, vocab // 2, vocab - 1])
+    rows = torch.randn(4, dim, generator=torch.Generator().manual_seed(1)).bfloat16()
+    rows[3] = rows[1]
+    weight[ids.cuda()] = rows.cuda()
+    out = torch.empty(4, dim, dtype=torch.bfloat16, device="cuda")
+    tcuscan.embedding(ids.cuda(), weight, out)
+    ws = tcuscan.new_embedding_backward_workspace(4, vocab, dim)
+    tcuscan.embedding_backward(ids.cuda(), out, weight, ws=ws)
+    torch.cuda.synchronize()
+    assert torch.equal(out.cpu(), rows)
+    want = {0: rows[0], vocab // 2: rows[2], vocab - 1: (rows[1].float() * 2).bfloat16()}
+    for r, w in want.items():
+        assert torch.equal(weight[r].cpu(), w)
+    assert int((weight != 0).any(1).sum()) == 3
+
+
+@pytest.mark.parametrize("n", [4095, 4096, 4097, 4160])
+def test_gradient_on_both_sides_of_the_choice_of_form(n):
+    check_gradient(zipf(n, 3000, 30 + n), 3000, 24, "bf16", "f32")
+    check_gradient([11] * n, 64, 40, "f16", "f16", accumulate=True)
