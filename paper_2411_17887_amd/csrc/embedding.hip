@@ -127,7 +127,7 @@ struct GradArgs {
     float *partial;
     size_t n, vocab, dim, out_stride, weight_stride;
     long long padding;
-    size_t piece, slices, piece_groups, zero_groups, rows;      // rows: of the table to a workgroup, where there are few tokens
+    size_t slices, piece_groups, zero_groups, rows;      // rows: of the table to a workgroup, where there are few tokens
     float scale;
     int wide_ids, accumulate;
 };
@@ -143,25 +143,28 @@ __global__ __launch_bounds__(kThreads) void token_keys_kernel(GradArgs A)
     A.tokens[t] = (uint32_t)t;
 }
 
-// Few tokens: no sort.  A workgroup takes `rows` rows of the table and a slice of the columns.  Each of its wavefronts looks a quarter of the token numbers over
-// and lists those of its rows in order, then sums them row by row; a row that several quarters have is put together in LDS, in the order of the
-// quarters.  One launch, whose time is that of its dependent steps: the numbers, a gradient's rows eight at a time, the table's row.
-constexpr int kFewTokens = 4096, kMaxFewRows = 64, kWaves = kThreads / 64, kQuarter = kFewTokens / kWaves;
-template <int DG, int DW, bool ALIGNED> __global__ __launch_bounds__(kThreads) void few_tokens_kernel(GradArgs A)
+// Few tokens: no sort.  A workgroup takes `rows` rows of the table and a slice of the columns.  Each of its wavefronts looks an eighth of the token numbers over
+// and lists those of its rows in order, then sums them row by row; a row that several eighths have is put together in LDS, in their order.
+// One launch, whose time is that of its dependent steps: the numbers, a gradient's rows eight at a time, the table's row: 3001 tokens of 1000 numbers and
+// 512 columns take 13 us.  It grows with the tokens of the most frequent number, the sort and its launches do not: 4096 tokens take 20 us here and 30 there
+// where 32000 numbers share them, 62 and 27 where all have the same, and twice as many 28 and 34, 117 and 31.
+constexpr int kFewTokens = 4096, kMaxFewRows = 64, kWaves = 8, kShare = kFewTokens / kWaves;
+template <int DG, int DW, bool ALIGNED> __global__ __launch_bounds__(64 * kWaves) void few_tokens_kernel(GradArgs A)
 {
     typedef Lane<DG, DW, ALIGNED> L;
     typedef typename L::G G;
     typedef typename Elem<DW>::T W;
-    __shared__ uint32_t list[kWaves][kQuarter];    // (row of the workgroup) << 16 | token
-    __shared__ uint64_t rows_of[kWaves];           // rows that a quarter has
-    __shared__ float part[2][kWaves][L::N * 64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    __shared__ uint32_t list[kWaves][kShare];      // (row of the workgroup) << 16 | token
+    __shared__ uint64_t rows_of[kWaves];             // rows that a share of the tokens has
+    __shared__ float part[kWaves][L::N * 64];
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const unsigned lane = threadIdx.x & 63;
     const size_t first = blockIdx.x / A.slices * A.rows, c0 = blockIdx.x % A.slices * L::kSlice;
     const size_t last = first + A.rows < A.vocab ? first + A.rows : A.vocab;
     int listed = 0;
     uint64_t mine = 0;
     {
-        const size_t quarter = ((A.n + kWaves - 1) / kWaves + 63) & ~(size_t)63, begin = wave * quarter, end = begin + quarter < A.n ? begin + quarter : A.n;
+        const size_t share = ((A.n + kWaves - 1) / kWaves + 63) & ~(size_t)63, begin = wave * share, end = begin + share < A.n ? begin + share : A.n;
         constexpr int kAhead = 8;
         for (size_t t0 = begin; t0 < end; t0 += 64 * kAhead) {
             long long id[kAhead];
@@ -202,54 +205,71 @@ template <int DG, int DW, bool ALIGNED> __global__ __launch_bounds__(kThreads) v
             while (votes) {
                 constexpr int kAhead = 8;
                 typename L::Vec v[kAhead];
-                int count = 0;
 #pragma unroll
                 for (int u = 0; u < kAhead; ++u) {
-                    if (!votes) break;
-                    const int source = __builtin_ctzll(votes);
+                    v[u] = typename L::Vec{};
+                    if (votes) v[u] = L::load((const G *)A.d_out + (size_t)(__builtin_amdgcn_readlane((int)item, __builtin_ctzll(votes)) & 0xFFFF) * A.out_stride, c0, A.dim, lane);
                     votes &= votes - 1;
-                    count = u + 1;
-                    v[u] = L::load((const G *)A.d_out + (size_t)(__builtin_amdgcn_readlane((int)item, source) & 0xFFFF) * A.out_stride, c0, A.dim, lane);
                 }
 #pragma unroll
-                for (int u = 0; u < kAhead; ++u)
-                    if (u < count) L::add(sum, v[u]);
+                for (int u = 0; u < kAhead; ++u) L::add(sum, v[u]);
             }
         }
     };
     const int rows = (int)(last - first);
-    for (int row = 0; row < rows; ++row) {         // rows of one quarter, and of none
-        const bool own = has >> row & 1 && !(several >> row & 1), empty = !(any >> row & 1) && row % kWaves == wave && !A.accumulate;
-        if (!own && !empty) continue;
+    if (!A.accumulate) {                           // rows of none, all of them together
+        const unsigned columns = (unsigned)(A.dim - c0 < L::kSlice ? A.dim - c0 : L::kSlice);
+        if constexpr (ALIGNED) {
+            typedef W Group __attribute__((ext_vector_type(L::kGroup)));
+            const unsigned width = columns / L::kGroup;
+            for (unsigned i = threadIdx.x; i < rows * width; i += 64 * kWaves) {
+                const unsigned row = i / width;
+                if (!(any >> row & 1)) *(Group *)(table + row * A.weight_stride + c0 + (i - row * width) * L::kGroup) = Group{};
+            }
+        } else {                                   // 16 bytes at a time between a row's first and last boundary of 16
+            for (int row = wave; row < rows; row += kWaves) {
+                if (any >> row & 1) continue;
+                W *const to = table + (size_t)row * A.weight_stride + c0;
+                constexpr unsigned kWide = 16 / sizeof(W);
+                unsigned lead = (unsigned)(-(uintptr_t)to & 15) / sizeof(W);
+                if (lead > columns) lead = columns;
+                const unsigned wide = (columns - lead) / kWide, rest = lead + wide * kWide;
+                if (lane < lead) to[lane] = W(0);
+                for (unsigned i = lane; i < wide; i += 64) *(uint4 *)(to + lead + i * kWide) = uint4{};
+                if (rest + lane < columns) to[rest + lane] = W(0);
+            }
+        }
+    }
+    for (uint64_t left = has & ~several; left; left &= left - 1) {        // rows of this share alone
+        const int row = __builtin_ctzll(left);
         float sum[L::N] = {};
-        if (own) sum_row(row, sum);
+        sum_row(row, sum);
         L::template finish<DW>(table + (size_t)row * A.weight_stride, c0, A.dim, lane, sum, A.scale, A.accumulate);
     }
-    int turn = 0;
-    for (uint64_t left = several; left; left &= left - 1, turn ^= 1) {
+    for (uint64_t left = several; left; left &= left - 1) {
         const int row = __builtin_ctzll(left);
         float sum[L::N] = {};
         if (has >> row & 1) sum_row(row, sum);
+        __syncthreads();                           // (the row before has been read)
 #pragma unroll
-        for (int k = 0; k < L::N; ++k) part[turn][wave][k * 64 + lane] = sum[k];
-        __syncthreads();                           // (the other half is free for the next row: its readers have passed the barrier before)
-        if (row % kWaves == wave) {
+        for (int k = 0; k < L::N; ++k) part[wave][k * 64 + lane] = sum[k];
+        __syncthreads();
+        if (row % kWaves != wave) continue;
 #pragma unroll
-            for (int k = 0; k < L::N; ++k) {
-                sum[k] = part[turn][0][k * 64 + lane];
+        for (int k = 0; k < L::N; ++k) {
+            sum[k] = part[0][k * 64 + lane];
 #pragma unroll
-                for (int w = 1; w < kWaves; ++w) sum[k] += part[turn][w][k * 64 + lane];
-            }
-            L::template finish<DW>(table + (size_t)row * A.weight_stride, c0, A.dim, lane, sum, A.scale, A.accumulate);
+            for (int w = 1; w < kWaves; ++w) sum[k] += part[w][k * 64 + lane];
         }
+        L::template finish<DW>(table + (size_t)row * A.weight_stride, c0, A.dim, lane, sum, A.scale, A.accumulate);
     }
 }
 
-// Many tokens.  The sorted pairs are cut into pieces of `piece` pairs, whatever runs they hold, so that a frequent token's run is shared by many
+// Many tokens.  The sorted pairs are cut into pieces of 32 pairs, whatever runs they hold, so that a frequent token's run is shared by many
 // wavefronts: a wavefront takes a piece and a slice of the columns.  Runs that lie inside a piece are finished there; what a piece has of
 // a run that goes on beyond it is kept, in fp32, in one of the piece's two places (0: the run comes from the piece before, 1: it starts here)
 // and added up, piece by piece in their order, by join_runs_kernel.  Every second workgroup, as long as both are left, writes zeros into rows that no token took.
-constexpr int kMaxPiece = 32, kZeroRows = 64;
+constexpr int kPiece = 32, kZeroRows = 64;
 template <int DG, int DW, bool ALIGNED> __global__ __launch_bounds__(kThreads) void sum_runs_kernel(GradArgs A)
 {
     typedef Lane<DG, DW, ALIGNED> L;
@@ -279,9 +299,9 @@ template <int DG, int DW, bool ALIGNED> __global__ __launch_bounds__(kThreads) v
         return;
     }
     const size_t item = index * (kThreads / 64) + wave, piece = item / A.slices, c0 = item % A.slices * L::kSlice;
-    const size_t begin = piece * A.piece;
+    const size_t begin = piece * kPiece;
     if (begin >= A.n) return;
-    const int count = (int)(begin + A.piece < A.n ? A.piece : A.n - begin);
+    const int count = (int)(begin + kPiece < A.n ? kPiece : A.n - begin);
     // lane i: the piece's i-th pair; lane 62: the key in front, 63: the one behind (none there: one that no pair has)
     const uint32_t none = 0xFFFFFFFFu;
     uint32_t key = none, token = 0;
@@ -331,11 +351,11 @@ template <int DW, int VEC> __global__ __launch_bounds__(64 * kJoinWaves) void jo
     typedef typename Elem<DW>::T W;
     typedef float Vec __attribute__((ext_vector_type(VEC)));
     typedef W WVec __attribute__((ext_vector_type(VEC)));
-    const size_t slices = (A.dim + 64 * VEC - 1) / (64 * VEC), piece = blockIdx.x / slices, behind = (piece + 1) * A.piece;
+    const size_t slices = (A.dim + 64 * VEC - 1) / (64 * VEC), piece = blockIdx.x / slices, behind = (piece + 1) * kPiece;
     if (behind >= A.n) return;
     const uint32_t row = A.keys[behind];
     if (A.keys[behind - 1] != row || row >= A.vocab) return;
-    if (piece > 0 && A.keys[piece * A.piece] == row && A.keys[piece * A.piece - 1] == row) return;      // (the run started before)
+    if (piece > 0 && A.keys[piece * kPiece] == row && A.keys[piece * kPiece - 1] == row) return;      // (the run started before)
     __shared__ size_t end;
     __shared__ Vec sums[kJoinWaves][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -345,7 +365,7 @@ template <int DW, int VEC> __global__ __launch_bounds__(64 * kJoinWaves) void jo
             const size_t mid = lo + (hi - lo) / 2;
             if (A.keys[mid] <= row) lo = mid + 1; else hi = mid;
         }
-        end = (lo - 1) / A.piece + 1;              // the piece behind the run's last
+        end = (lo - 1) / kPiece + 1;              // the piece behind the run's last
     }
     __syncthreads();
     const size_t count = end - piece, each = (count + kJoinWaves - 1) / kJoinWaves;
@@ -395,9 +415,6 @@ template <int G, int W> struct FewAligned { static const void *fn() { return (co
 template <int G, int W> struct Runs { static const void *fn() { return (const void *)sum_runs_kernel<G, W, false>; } };
 template <int G, int W> struct RunsAligned { static const void *fn() { return (const void *)sum_runs_kernel<G, W, true>; } };
 
-// Pairs to a piece.
-size_t piece_for(size_t) { return kMaxPiece; }
-
 // What the gradient's workspace holds, in bytes from its start.
 struct GradLayout {
     size_t chain, keys, keys_tmp, tokens, tokens_tmp, flags, positions, partial, all;
@@ -414,7 +431,7 @@ struct GradLayout {
         positions = tokens_tmp + words;
         flags = positions + words;
         partial = (flags + n + 255) / 256 * 256;
-        all = partial + 2 * ((n + piece_for(n) - 1) / piece_for(n)) * dim * 4;
+        all = partial + 2 * ((n + kPiece - 1) / kPiece) * dim * 4;
     }
 };
 
@@ -485,7 +502,7 @@ tcuscan_status_t tcuscan_embedding_backward(const void *d_ids, int id_bytes, siz
         const size_t groups = (vocab + A.rows - 1) / A.rows * A.slices;
         if (groups > kMostRows) return TCUSCAN_ERR_UNSUPPORTED;
         const void *fn = aligned ? pick<FewAligned>(out_dt, weight_dt) : pick<Few>(out_dt, weight_dt);
-        return hipLaunchKernel(fn, dim3((unsigned)groups), dim3(kThreads), args, 0, s) == hipSuccess ? TCUSCAN_OK : TCUSCAN_ERR_HIP;
+        return hipLaunchKernel(fn, dim3((unsigned)groups), dim3(64 * kWaves), args, 0, s) == hipSuccess ? TCUSCAN_OK : TCUSCAN_ERR_HIP;
     }
     if (hipLaunchKernel((const void *)token_keys_kernel, dim3((unsigned)((n + kThreads - 1) / kThreads)), dim3(kThreads), args, 0, s) != hipSuccess) return TCUSCAN_ERR_HIP;
     int bits = 0;
@@ -493,9 +510,8 @@ tcuscan_status_t tcuscan_embedding_backward(const void *d_ids, int id_bytes, siz
     const tcuscan_status_t st = tcuscan_split_radix_sort_u32(A.keys, A.tokens, n, bits, ws + L.keys_tmp, ws + L.tokens_tmp, ws + L.flags, ws + L.positions,
                                                              d_ws, L.chain, stream);
     if (st != TCUSCAN_OK) return st;
-    A.piece = piece_for(n);
     A.slices = (dim + 64 * cols - 1) / (64 * cols);
-    const size_t pieces = (n + A.piece - 1) / A.piece, zero_groups = accumulate ? 0 : (vocab + kZeroRows - 1) / kZeroRows;
+    const size_t pieces = (n + kPiece - 1) / kPiece, zero_groups = accumulate ? 0 : (vocab + kZeroRows - 1) / kZeroRows;
     A.zero_groups = zero_groups;
     A.piece_groups = (pieces * A.slices + kThreads / 64 - 1) / (kThreads / 64);
     if (A.piece_groups + zero_groups > kMostRows) return TCUSCAN_ERR_UNSUPPORTED;
