@@ -392,7 +392,7 @@ struct StateShape {
     }
 };
 // (a workgroup's share of the registers: 256 rows of a state and 32 columns to a wavefront do not fit them)
-__host__ __device__ inline StateShape state_shape(unsigned A, unsigned E) { return {A <= 32 ? 32u : A <= 64 ? 64u : A <= 128 ? 128u : 256u, E <= 64 || A > 128 ? 1u : 2u}; }
+__host__ __device__ inline StateShape state_shape(unsigned A, unsigned E) { return {A <= 32 ? 32u : A <= 64 ? 64u : A <= 96 ? 96u : A <= 128 ? 128u : A <= 192 ? 192u : 256u, E <= 64 || A > 128 ? 1u : 2u}; }
 
 // The 4 x 4 square that four lanes side by side hold, transposed.
 __device__ __forceinline__ f32x4 turned(f32x4 v, int lane)
@@ -446,19 +446,22 @@ template <int AP, int CT, bool OUT, class P> __device__ __forceinline__ void mov
         }
 }
 
+// Columns of a tile of AP features: a power of two, for the permutation of granules.
+constexpr int tile_columns(int AP) { return AP <= 32 ? 32 : AP <= 64 ? 64 : AP <= 128 ? 128 : 256; }
+
 // READS: writes outputs and, of a row's last segment, the state.  Otherwise only what each segment but the last adds to the state.
 template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bounds__(64 * kWalkWaves, groups_at_once(AP)) void walk_kernel(WalkArgs W)
 {
     typedef typename Elem<DT>::T T;
-    constexpr int N = parts_of(DT), C = kBlock, EB = 16 * kWalkWaves * CT, kThreads = 64 * kWalkWaves;
+    constexpr int N = parts_of(DT), C = kBlock, LP = tile_columns(AP), EB = 16 * kWalkWaves * CT, kThreads = 64 * kWalkWaves;
     constexpr bool kDirectly = way_of(DT, WHOLE) == kDirect;
     constexpr int kTiles = 2, kOrder = N == 3 ? 3 : 2;         // tiles of 16 tokens
-    typedef Stage<DT, C, AP, kThreads, WHOLE> StageA;
+    typedef Stage<DT, C, LP, kThreads, WHOLE> StageA;
     typedef Stage<DT, C, EB, kThreads, WHOLE> StageE;
     // Loads that write LDS themselves go round kRing tiles of each array: while a block is worked on, the kRing - 1 behind it are on their way.
     constexpr int kRing = !kDirectly ? 1 : READS ? 3 : 4, kLoads = (READS ? 2 : 1) * StageA::kSure + StageE::kSure;
     // (Each tile is an array of its own: the compiler has a wavefront wait for loads into an array before it reads from it.)
-    constexpr int kX = READS ? N * C * AP : 8, kY = N * C * AP, kZ = N * C * EB, kNone = 8;
+    constexpr int kX = READS ? N * C * LP : 8, kY = N * C * LP, kZ = N * C * EB, kNone = 8;
     __shared__ __attribute__((aligned(16))) bf16_t sx0[kX], sx1[kRing > 1 ? kX : kNone], sx2[kRing > 2 ? kX : kNone];
     __shared__ __attribute__((aligned(16))) bf16_t sy0[kY], sy1[kRing > 1 ? kY : kNone], sy2[kRing > 2 ? kY : kNone], sy3[kRing > 3 ? kY : kNone];
     __shared__ __attribute__((aligned(16))) bf16_t sz0[kZ], sz1[kRing > 1 ? kZ : kNone], sz2[kRing > 2 ? kZ : kNone], sz3[kRing > 3 ? kZ : kNone];
@@ -563,7 +566,7 @@ template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bo
     auto take_block = [&](bf16_t *x_now, bf16_t *x_free, bf16_t *y_now, bf16_t *y_free, bf16_t *z_now, bf16_t *z_free) __attribute__((always_inline)) {
         const long long behind = length - at - C;
         const int n = tokens(length - at);
-        const int row_at = here(row_lane<AP>(lane)), y_at = here(column_lane<AP, 8>(lane, 0)), z_at = here(column_lane<EB, 4 * CT>(lane, wave_e));
+        const int row_at = here(row_lane<LP>(lane)), y_at = here(column_lane<LP, 8>(lane, 0)), z_at = here(column_lane<EB, 4 * CT>(lane, wave_e));
         if constexpr (kDirectly) {
             // of the loads behind this block's, as many may be on their way as there surely are (stores are waited for with them)
             if (kRing > 3 && behind > C) __builtin_amdgcn_s_waitcnt(loads_left((kRing > 3 ? 2 : 1) * kLoads));
@@ -614,8 +617,8 @@ template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bo
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
                     for (int i = 0; i < N; ++i) {
-                        queries[t].p[i] = row_operand<AP>(x_now + i * C * AP, row_at, 16 * t, 32 * s);
-                        keys[t].p[i] = row_operand<AP>(y_now + i * C * AP, row_at, 16 * t, 32 * s);
+                        queries[t].p[i] = row_operand<LP>(x_now + i * C * LP, row_at, 16 * t, 32 * s);
+                        keys[t].p[i] = row_operand<LP>(y_now + i * C * LP, row_at, 16 * t, 32 * s);
                     }
                 if (s + 1 < AP / 32) split_m(s + 1);
                 products<kOrder>([&](int i, int j) {           // (independent ones behind each other)
@@ -665,7 +668,7 @@ template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bo
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int m = 0; m < N; ++m) yt[t / 2 & 1][u].p[m] = column_operand<AP>(y_now + m * C * AP, y_at, 16 * t + 4 * u);
+                for (int m = 0; m < N; ++m) yt[t / 2 & 1][u].p[m] = column_operand<LP>(y_now + m * C * LP, y_at, 16 * t + 4 * u);
         };
         load_y(0);
 #pragma unroll
@@ -691,7 +694,7 @@ template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bo
                 for (int t = 0; t < AP / 16; ++t)
 #pragma unroll
                     for (int m = 0; m < N; ++m) {
-                        const bf16x8 y_part = column_operand<AP>(y_now + m * C * AP, y_at, 32 * (t / 2) + 4 * (t & 1));
+                        const bf16x8 y_part = column_operand<LP>(y_now + m * C * LP, y_at, 32 * (t / 2) + 4 * (t & 1));
 #pragma unroll
                         for (int c = 0; c < CT; ++c) M[t][c] = mfma(y_part, third[c].p[2 - m], M[t][c]);
                     }
@@ -945,8 +948,14 @@ Heads heads_of(const void *data, long long token, long long head, long long head
 
 template <int DT, int CT, bool WHOLE, bool READS> const void *walk_for(unsigned A)
 {
-    return A <= 32 ? (const void *)walk_kernel<DT, 32, CT, WHOLE, READS> : A <= 64 ? (const void *)walk_kernel<DT, 64, CT, WHOLE, READS>
-         : A <= 128 ? (const void *)walk_kernel<DT, 128, CT, WHOLE, READS> : (const void *)walk_kernel<DT, 256, 1, WHOLE, READS>;
+    switch (state_shape(A, 1).AP) {
+        case 32: return (const void *)walk_kernel<DT, 32, CT, WHOLE, READS>;
+        case 64: return (const void *)walk_kernel<DT, 64, CT, WHOLE, READS>;
+        case 96: return (const void *)walk_kernel<DT, 96, CT, WHOLE, READS>;
+        case 128: return (const void *)walk_kernel<DT, 128, CT, WHOLE, READS>;
+        case 192: return (const void *)walk_kernel<DT, 192, 1, WHOLE, READS>;
+        default: return (const void *)walk_kernel<DT, 256, 1, WHOLE, READS>;
+    }
 }
 template <int DT, int CT, bool READS> const void *walk_for(unsigned A, bool whole) { return whole ? walk_for<DT, CT, true, READS>(A) : walk_for<DT, CT, false, READS>(A); }
 template <int DT, bool READS> const void *walk_for(unsigned A, bool whole, unsigned CT) { return CT == 1 ? walk_for<DT, 1, READS>(A, whole) : walk_for<DT, 2, READS>(A, whole); }
