@@ -143,8 +143,9 @@ constexpr int parts_of(int dt) { return dt == kBF16 ? 1 : dt == kF16 ? 2 : 3; }
 constexpr int kBlock = 32;
 
 constexpr int kWalkWaves = 4;
-// Workgroups on a compute unit, by what LDS and registers give.
-constexpr int groups_at_once(int ap) { return ap > 128 ? 1 : 2; }
+// Workgroups on a compute unit, by what LDS and registers give.  States of 128 x 128 with their products of fp32's six pairs of parts need more than half of a
+// lane's registers: 20011 tokens of 8 heads take 285 us with one workgroup, 341 with two whose values are in part kept in memory.
+constexpr int groups_at_once(int dt, int ap, int ct, bool reads) { return ap > 128 || (dt == kF32 && ap == 128 && ct == 2 && reads) ? 1 : 2; }
 // s_waitcnt: no more than n loads and stores on their way, whatever else is.
 constexpr int loads_left(int n) { return (n & 15) | (n >> 4) << 14 | 0x0F70; }
 
@@ -450,7 +451,7 @@ template <int AP, int CT, bool OUT, class P> __device__ __forceinline__ void mov
 constexpr int tile_columns(int AP) { return AP <= 32 ? 32 : AP <= 64 ? 64 : AP <= 128 ? 128 : 256; }
 
 // READS: writes outputs and, of a row's last segment, the state.  Otherwise only what each segment but the last adds to the state.
-template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bounds__(64 * kWalkWaves, groups_at_once(AP)) void walk_kernel(WalkArgs W)
+template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bounds__(64 * kWalkWaves, groups_at_once(DT, AP, CT, READS)) void walk_kernel(WalkArgs W)
 {
     typedef typename Elem<DT>::T T;
     constexpr int N = parts_of(DT), C = kBlock, LP = tile_columns(AP), EB = 16 * kWalkWaves * CT, kThreads = 64 * kWalkWaves;
@@ -580,6 +581,12 @@ template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bo
         }
         __syncthreads();
         if constexpr (kDirectly) load(x_free, y_free, z_free);
+        if constexpr (AP <= 128)
+            if (e0 + wave_e >= (int)W.E) {         // a wavefront of no columns only loads (96 columns: 3 % less; with larger states the branch costs as much)
+                if constexpr (!kDirectly) load(x_now, y_now, z_now);
+                at += C;
+                return;
+            }
         Parts<N> zt[CT];                           // 16 columns of Z by 32 tokens
 #pragma unroll
         for (int c = 0; c < CT; ++c)
