@@ -379,8 +379,9 @@ tcuscan_status_t tcuscan_set_sort_fusion(int fused);
  *              aligned, zero-filled once.  An offset or slot out of range sets its fault word to 2
  *              (tcuscan_workspace_fault); nothing outside the arrays is touched then, and the results are unspecified.
  *
- * Inputs must be finite.  A value that is not spoils outputs of its own row and heads, also up to 63 tokens in front of it, and none
- * of other rows.  16-bit outputs are rounded once from fp32 sums; what the products round on the way is at most as much again.
+ * Inputs must be finite.  A value that is not spoils outputs of its own row and heads, also up to 31 tokens in front of it, and none
+ * of other rows.  What the products round on the way is
+ * far below the last bit of 16-bit outputs, and in fp32 about that of fp32 sums.
  */
 typedef struct {
     long long rows, total, heads, dk, dv;
@@ -428,10 +429,10 @@ tcuscan_status_t tcuscan_embedding(const void *d_ids, int id_bytes, size_t n, co
 
 /*
  * Its gradient by the table: d_weight_grad[r] = scale * (the sum of d_out_grad[t] over the tokens t with d_ids[t] == r), the sums in
- * fp32 and in an order that the sorted tokens alone fix (the same bits on every run).  Every row is written, zeros where no token is; with
+ * fp32 and in an order that the token numbers alone fix (the same bits on every run).  Every row is written, zeros where no token is; with
  * TCUSCAN_ACCUMULATE the sums are added to what is there, and rows without a token are not touched.  Tokens whose number is
- * negative, not below vocab (fault word 2) or equal to `padding` (-1: none) add nothing.  The tokens are sorted by their numbers with
- * tcuscan_split_radix_sort_u32.  n < 2^32.
+ * negative, not below vocab (fault word 2) or equal to `padding` (-1: none) add nothing.  More than 4096 tokens are sorted by
+ * their numbers with tcuscan_split_radix_sort_u32.  n < 2^32.
  *   d_ws       tcuscan_embedding_backward_workspace_bytes(n, vocab, dim) bytes, 16-byte aligned, zero-filled once
  */
 #define TCUSCAN_ACCUMULATE 1u

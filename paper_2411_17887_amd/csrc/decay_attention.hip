@@ -911,17 +911,25 @@ tcuscan_status_t check_shape(const tcuscan_attention_shape_t *p, int dt)
     return TCUSCAN_OK;
 }
 
-// Rows are cut into segments so that a call with few rows and heads still has a workgroup or two for every compute unit, but not below 128 tokens; calls
-// of up to 512 tokens are not cut (three launches then take longer than eight blocks in a row).
-constexpr size_t kWantedGroups = 512;
-constexpr unsigned kMinSegmentLog2 = 7, kWholeRows = 62;
-constexpr long long kMostUncut = 512;
+// Rows are cut into segments so that a call with few rows and heads still has work for the whole chip.  Each segment costs a state written and read, and a
+// step of join_kernel.
+//   * Not cut: calls of up to 256 tokens (8 heads of 64: 16 us against 20 in three launches; 512 tokens 26 against 19, their gradients 71 against 41).
+//   * 64 tokens a segment while these are no more workgroups than compute units (gradients of 512 tokens, 8 heads of 64: 41 us, with 128 tokens 47; but
+//     5000 tokens in 3 rows 38, with 128 tokens 31).
+//   * Then 128 or more, for 512 workgroups (65536 tokens, 16 heads of 128: 382 us, with 256 workgroups 431, with 1024 407), or 1024 where both sides of the
+//     state are at most 64, of which more fit a unit (20000 tokens in 60 rows, 16 heads of 64: 82 us, with 512 104), and eight heads or more share the
+//     workgroups, or there would be too many segments in a row (30000 tokens of 4 heads of 48: 77, with 512 55).
+constexpr size_t kUnits = 256, kWantedGroups = 512;
+constexpr unsigned kWholeRows = 62;
+constexpr long long kMostUncut = 256;
 unsigned segment_log2_for(const tcuscan_attention_shape_t &s)
 {
     if (s.total <= kMostUncut) return kWholeRows;
-    const size_t blocks = (size_t)((s.dk > s.dv ? s.dk : s.dv) + 127) / 128;
-    unsigned log2 = kMinSegmentLog2;
-    while (((size_t)s.total * s.heads * blocks) >> log2 > kWantedGroups) ++log2;
+    const long long larger = s.dk > s.dv ? s.dk : s.dv;
+    const size_t work = (size_t)s.total * s.heads * ((size_t)(larger + 127) / 128), wanted = larger <= 64 && s.heads >= 8 ? 2 * kWantedGroups : kWantedGroups;
+    if (work >> 6 <= kUnits) return 6;
+    unsigned log2 = 7;
+    while (work >> log2 > wanted) ++log2;
     return (size_t)s.total >> log2 ? log2 : kWholeRows;
 }
 size_t pieces_for(const tcuscan_attention_shape_t &s, unsigned segment_log2) { return (size_t)s.rows + ((size_t)s.total >> segment_log2); }
