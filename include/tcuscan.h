@@ -380,8 +380,8 @@ tcuscan_status_t tcuscan_set_sort_fusion(int fused);
  *              (tcuscan_workspace_fault); nothing outside the arrays is touched then, and the results are unspecified.
  *
  * Inputs must be finite.  A value that is not spoils outputs of its own row and heads, also up to 31 tokens in front of it, and none
- * of other rows.  What the products round on the way is
- * far below the last bit of 16-bit outputs, and in fp32 about that of fp32 sums.
+ * of other rows.  What the products round on the way is far below the last bit of 16-bit outputs, and in fp32 about what fp32
+ * sums round.
  */
 typedef struct {
     long long rows, total, heads, dk, dv;

@@ -117,8 +117,13 @@ __device__ __forceinline__ long long state_of(const long long *slots, unsigned r
 // M += Y^T (wZ).  A wavefront owns 16 CT columns of Z, out and M and all A rows of M, in MFMA accumulators from the first token to the
 // last.  The products are ordered so that operands fall into the lanes that have them: the accumulators of M, two row tiles side by side, are
 // the left operand of M^T X^T as they stand (tile rows are dealt so that a lane's eight values are eight consecutive a), and Z's columns are
-// read transposed once, for Z^T P^T and, weighted, for the update.  Only X, Y and Z, which all
-// wavefronts of a workgroup share, go through LDS.
+// read transposed once, for Z^T P^T and, weighted, for the update.  Only X, Y and Z, which all wavefronts of a workgroup share, go through LDS.
+//
+// What it costs.  A row of many tokens is cut into segments, so Y and Z are read twice: once for what each segment adds to the state, then, with what
+// each segment starts from (join_kernel), for the outputs.  65536 bf16 tokens, 16 heads of 128 x 128 (inputs and outputs 1.08 GB, 1.61 GB moved): 117 us for the
+// first reading (4.6 TB/s, a large copy's rate), 14 for the join, 250 for the outputs (4.3 TB/s); with all inputs in L2 77 and 195.  Memory bounds it, then
+// the matrix unit, which is busy a third of the time.  f16 and fp32 multiply three and six pairs of parts and are bound by the matrix unit and by splitting:
+// 20011 f16 tokens, 16 heads of 80 x 96, 81 + 10 + 158 us.  In short rows the time is that of blocks in a row, 2 us each.
 //
 // Precision.  The matrix unit multiplies bf16 and adds in fp32, so every operand is a sum of bf16 parts: bf16 inputs one, f16 two (exact),
 // fp32 three.  What is rounded on the way:
@@ -139,7 +144,7 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int parts_of(int dt) { return dt == kBF16 ? 1 : dt == kF16 ? 2 : 3; }
 // Tokens of a block.  With 64 the state would be read (split, multiplied) half as often, but LDS would hold no more than the next block beside the present
-// one: too little on its way to keep the memory busy (65536 tokens 400 us, of which the reading of inputs from L2 alone 300).
+// one: too little on its way to keep the memory busy (65536 tokens 400 us, and 300 with all inputs in L2; with 32 tokens 382 and 286).
 constexpr int kBlock = 32;
 
 constexpr int kWalkWaves = 4;
@@ -227,7 +232,7 @@ template <class T> __device__ __forceinline__ T here(T v)
 // on become zeros.  Three ways:
 //   kDirect   bf16, granules aligned and either inside or outside: loads that write LDS themselves, lane after lane, so that it is the lanes' addresses
 //             that are permuted; what is outside is beyond the end of the buffer they read from.  They need no registers while they are on
-//             their way (held there, the 48 a lane would need at dk = dv = 128 are spilled).
+//             their way (the 48 a lane would need at dk = dv = 128 do not fit beside the state and are spilled).
 //   kStaged   fp32 and f16, granules as above: through registers, split into parts on the way.
 //   kSlow     anything else: element by element.
 enum Way { kDirect, kStaged, kSlow };
@@ -734,7 +739,9 @@ template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bo
     }
 }
 
-// What each segment of a row starts from, from what the segments in front of it add: a thread takes four elements of the state along the row.
+// What each segment of a row starts from, from what the segments in front of it add: a thread takes four elements of the state along the row, four segments'
+// loads on their way at a time.  The carry across segments is a sum with one decay, so this is all that has to be done in order.  Bound by memory for many rows
+// (8 rows of 4096 tokens, 16 heads of 128 x 128: 16 us, 20 with the transposed states), by the steps in a row for few (65536 tokens in 32 segments: 14 us).
 constexpr int kJoinThreads = 256, kJoinAhead = 4;
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(WalkArgs W)
 {
@@ -805,7 +812,9 @@ template <int DT, int VEC> __global__ __launch_bounds__(kSumThreads) void sum_he
 }
 
 // One token for each of many sequences.  A workgroup takes a block of columns of one state: 2^lanes_log2 lanes to a row, VEC columns each, as many rows at
-// a time as the workgroup has lanes for.  The state is read and written once; nothing else counts.
+// a time as the workgroup has lanes for; the state stays in registers between its product with q and its writing.  The state is read and written once and
+// nothing else counts: 256 sequences of 16 heads of 128 x 128 (537 MB) take 112 us, 4.8 TB/s, a large copy's rate; one sequence, whose columns are spread over
+// as many workgroups as there are columns for, the time of a launch.
 struct StepArgs {
     Heads q, k, v, out;
     const float *log_decay;

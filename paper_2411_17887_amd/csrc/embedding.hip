@@ -2,10 +2,11 @@
 //
 //   lookup   : out[t] = scale * weight[id[t]]
 //   gradient : d_weight[r] = scale * (sum of d_out[t] over the t with id[t] = r, in ascending order of t)
-//              The (id, t) pairs are sorted by id (tcuscan_split_radix_sort_u32: stable, so t ascends within an id); a row's
-//              tokens then are one run of the sorted pairs.
+//              Few tokens: workgroups list those of their rows.  Many: the (id, t) pairs are sorted by id
+//              (tcuscan_split_radix_sort_u32: stable, so t ascends within an id); a row's tokens then are one run of the sorted pairs.
 //
-// Sums are held in 32 bits and rounded once to the table's type.  Both move bytes and compute next to nothing.
+// Sums are held in 32 bits, put together from parts in an order that the token numbers alone fix, and rounded once to the table's type.  Both move
+// bytes and compute next to nothing.
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -93,7 +94,8 @@ template <int DG, int DOTHER, bool ALIGNED> struct Lane {
 };
 
 // A wavefront takes a slice of the columns of kTokens tokens: their loads are on their way together.  (kTokens = 1: few tokens, whose columns are spread
-// over as many wavefronts as there are.)
+// over as many wavefronts as there are.)  Bound by memory: 65536 bf16 rows of 1024 from an fp32 table (74 MB of it read, 134 MB written) take 43 us,
+// 4.8 TB/s; 24 rows of 2048 2.5 us, their loads one after the other: the number, the row.
 template <int DW, int DO, bool ALIGNED, int kTokens> __global__ __launch_bounds__(kThreads) void lookup_kernel(LookupArgs A)
 {
     typedef Lane<DW == kF32 ? DO : DW, DW == kF32 ? DW : DO, ALIGNED> L;       // (eight columns to a lane unless both types are fp32)
@@ -146,7 +148,7 @@ __global__ __launch_bounds__(kThreads) void token_keys_kernel(GradArgs A)
 // Few tokens: no sort.  A workgroup takes `rows` rows of the table and a slice of the columns.  Each of its wavefronts looks an eighth of the token numbers over
 // and lists those of its rows in order, then sums them row by row; a row that several eighths have is put together in LDS, in their order.
 // One launch, whose time is that of its dependent steps: the numbers, a gradient's rows eight at a time, the table's row: 3001 tokens of 1000 numbers and
-// 512 columns take 13 us.  It grows with the tokens of the most frequent number, the sort and its launches do not: 4096 tokens take 20 us here and 30 there
+// 512 columns take 8 us, into 8000 rows of 515 15.  It grows with the tokens of the most frequent number, the sort and its launches do not: 4096 tokens take 20 us here and 30 there
 // where 32000 numbers share them, 62 and 27 where all have the same, and twice as many 28 and 34, 117 and 31.
 constexpr int kFewTokens = 4096, kMaxFewRows = 64, kWaves = 8, kShare = kFewTokens / kWaves;
 template <int DG, int DW, bool ALIGNED> __global__ __launch_bounds__(64 * kWaves) void few_tokens_kernel(GradArgs A)
@@ -155,7 +157,7 @@ template <int DG, int DW, bool ALIGNED> __global__ __launch_bounds__(64 * kWaves
     typedef typename L::G G;
     typedef typename Elem<DW>::T W;
     __shared__ uint32_t list[kWaves][kShare];      // (row of the workgroup) << 16 | token
-    __shared__ uint64_t rows_of[kWaves];             // rows that a share of the tokens has
+    __shared__ uint64_t rows_of[kWaves];           // rows that a share of the tokens has
     __shared__ float part[kWaves][L::N * 64];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const unsigned lane = threadIdx.x & 63;
@@ -269,6 +271,7 @@ template <int DG, int DW, bool ALIGNED> __global__ __launch_bounds__(64 * kWaves
 // wavefronts: a wavefront takes a piece and a slice of the columns.  Runs that lie inside a piece are finished there; what a piece has of
 // a run that goes on beyond it is kept, in fp32, in one of the piece's two places (0: the run comes from the piece before, 1: it starts here)
 // and added up, piece by piece in their order, by join_runs_kernel.  Every second workgroup, as long as both are left, writes zeros into rows that no token took.
+// Bound by memory: 65536 bf16 gradients of 1024 columns into 65536 fp32 rows (134 MB read, 268 written) take 97 us, 4.2 TB/s, after a sort of 35.
 constexpr int kPiece = 32, kZeroRows = 64;
 template <int DG, int DW, bool ALIGNED> __global__ __launch_bounds__(kThreads) void sum_runs_kernel(GradArgs A)
 {
@@ -344,7 +347,8 @@ template <int DG, int DW, bool ALIGNED> __global__ __launch_bounds__(kThreads) v
 }
 
 // The runs that lie in several pieces.  A workgroup looks at one piece and a slice of 64 VEC columns: if a run starts in it and goes on behind it, its wavefronts
-// take the pieces that hold it in turns of consecutive ones, and the first of them adds the others' sums.
+// take the pieces that hold it in turns of consecutive ones, and the first of them adds the others' sums.  Most pieces have nothing to do here; the rest of the
+// 14 us at 65536 tokens is the most frequent number's run.
 constexpr int kJoinWaves = 4;
 template <int DW, int VEC> __global__ __launch_bounds__(64 * kJoinWaves) void join_runs_kernel(GradArgs A)
 {
@@ -436,7 +440,9 @@ struct GradLayout {
 };
 
 constexpr size_t kMostRows = 0x7FFFFFFFu;
-constexpr size_t kManyItems = 1 << 14;      // wavefronts' items from which on each takes four tokens
+// Wavefronts' items from which on each takes four tokens: 32768 bf16 rows of 512 take 10.0 us, one token at a time 11.7; below, either is as fast but for single
+// tokens, which four at a time would give to one wavefront.
+constexpr size_t kManyItems = 1 << 14;
 
 }  // namespace
 

@@ -337,3 +337,29 @@ def test_inputs_shared_by_all_tokens_or_heads_without_copies():
     c.host = [x.double().cpu().numpy() for x in c.qkv]
     assert k.stride(0) == 0 and q.stride(1) == 0
     c.check_forward(*c.forward())
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dk,dv", [(96, 192), (192, 90), (70, 96), (130, 160)])
+def test_states_between_powers_of_two(kind, dk, dv):
+    """In one segment and in several; some wavefronts have no columns."""
+    for lengths in ([45, 3], [290, 20]):
+        c = Case(kind, lengths, heads=(2, 1, 2), dk=dk, dv=dv, seed=31)
+        c.check_forward(*c.forward())
+        c.check_backward(*c.backward())
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_gradients_of_shared_heads_of_any_size(kind):
+    for dk, dv, packed in ((13, 6, False), (12, 20, True), (12, 20, False)):
+        c = Case(kind, [90, 0, 7], heads=(2, 1, 2), all_heads=4, dk=dk, dv=dv, packed=packed, seed=32)
+        c.check_forward(*c.forward())
+        c.check_backward(*c.backward())
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("lengths", [[256], [257], [320], [64, 65, 63, 128], [1023], [2049], [1, 2100]], ids=str)
+def test_calls_around_the_choices_of_segments(kind, lengths):
+    c = Case(kind, lengths, heads=(8, 8, 8), dk=32, dv=48, seed=33)
+    c.check_forward(*c.forward())
+    c.check_backward(*c.backward())

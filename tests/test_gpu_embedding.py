@@ -228,3 +228,17 @@ def test_rows_further_apart_than_32_bits_reach():
 def test_gradient_on_both_sides_of_the_choice_of_form(n):
     check_gradient(zipf(n, 3000, 30 + n), 3000, 24, "bf16", "f32")
     check_gradient([11] * n, 64, 40, "f16", "f16", accumulate=True)
+
+
+@pytest.mark.parametrize("w_kind", KINDS)
+@pytest.mark.parametrize("dim", [1, 7, 9, 31, 513, 530])
+def test_rows_of_no_token_start_and_end_anywhere(dim, w_kind):
+    """Most rows are cleared 16 bytes at a time; they start and end at every element within 16 bytes."""
+    for pad in (0, 1, 3):
+        check_gradient([3, 40, 40, 199], 200, dim, "bf16", w_kind, pad=pad)
+
+
+@pytest.mark.parametrize("ids", [[4] * 4096, [4, 9] * 2048, [i % 8 for i in range(4096)], [1] * 512 + [2] * 1500 + [1] * 2, [3] * 513], ids=["one", "two", "eight", "shares", "edge"])
+def test_few_tokens_with_numbers_that_many_share(ids):
+    check_gradient(ids, 70, 72)
+    check_gradient(ids, 70, 19, "bf16", "f16", accumulate=True)
