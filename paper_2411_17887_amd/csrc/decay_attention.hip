@@ -922,7 +922,8 @@ tcuscan_status_t check_shape(const tcuscan_attention_shape_t *p, int dt)
 
 // Rows are cut into segments so that a call with few rows and heads still has work for the whole chip.  Each segment costs a state written and read, and a
 // step of join_kernel.
-//   * Not cut: calls of up to 256 tokens (8 heads of 64: 16 us against 20 in three launches; 512 tokens 26 against 19, their gradients 71 against 41).
+//   * Not cut: calls of up to 256 tokens to a row, as far as the host can tell: 256 for each row, 512 in all (256 tokens in one row, 8 heads of 64: 16 us against
+//     20 in three launches; 512 tokens 26 against 19, their gradients 71 against 41).
 //   * 64 tokens a segment while these are no more workgroups than compute units (gradients of 512 tokens, 8 heads of 64: 41 us, with 128 tokens 47; but
 //     5000 tokens in 3 rows 38, with 128 tokens 31).
 //   * Then 128 or more, for 512 workgroups (65536 tokens, 16 heads of 128: 382 us, with 256 workgroups 431, with 1024 407), or 1024 where both sides of the
@@ -930,10 +931,10 @@ tcuscan_status_t check_shape(const tcuscan_attention_shape_t *p, int dt)
 //     workgroups, or there would be too many segments in a row (30000 tokens of 4 heads of 48: 77, with 512 55).
 constexpr size_t kUnits = 256, kWantedGroups = 512;
 constexpr unsigned kWholeRows = 62;
-constexpr long long kMostUncut = 256;
+constexpr long long kMostUncutRow = 256, kMostUncut = 512;
 unsigned segment_log2_for(const tcuscan_attention_shape_t &s)
 {
-    if (s.total <= kMostUncut) return kWholeRows;
+    if (s.total <= kMostUncut && s.total <= kMostUncutRow * s.rows) return kWholeRows;
     const long long larger = s.dk > s.dv ? s.dk : s.dv;
     const size_t work = (size_t)s.total * s.heads * ((size_t)(larger + 127) / 128), wanted = larger <= 64 && s.heads >= 8 ? 2 * kWantedGroups : kWantedGroups;
     if (work >> 6 <= kUnits) return 6;
