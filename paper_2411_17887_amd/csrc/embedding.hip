@@ -148,8 +148,8 @@ __global__ __launch_bounds__(kThreads) void token_keys_kernel(GradArgs A)
 // Few tokens: no sort.  A workgroup takes `rows` rows of the table and a slice of the columns.  Each of its wavefronts looks an eighth of the token numbers over
 // and lists those of its rows in order, then sums them row by row; a row that several eighths have is put together in LDS, in their order.
 // One launch, whose time is that of its dependent steps: the numbers, a gradient's rows eight at a time, the table's row: 3001 tokens of 1000 numbers and
-// 512 columns take 8 us, into 8000 rows of 515 15.  It grows with the tokens of the most frequent number, the sort and its launches do not: 4096 tokens take 20 us here and 30 there
-// where 32000 numbers share them, 62 and 27 where all have the same, and twice as many 28 and 34, 117 and 31.
+// 512 columns take 8 us, into 8000 rows of 515 14.  It grows with the tokens of the most frequent number, the sort and its launches do not: 4096 tokens take 15 us here and 30 there
+// where 32000 numbers share them, 63 and 27 where all have the same (fp32, 512 columns); twice as many all the same would take 117 and 31.
 constexpr int kFewTokens = 4096, kMaxFewRows = 64, kWaves = 8, kShare = kFewTokens / kWaves;
 template <int DG, int DW, bool ALIGNED> __global__ __launch_bounds__(64 * kWaves) void few_tokens_kernel(GradArgs A)
 {
@@ -501,10 +501,11 @@ tcuscan_status_t tcuscan_embedding_backward(const void *d_ids, int id_bytes, siz
     const size_t cols = out_dt == kF32 ? kLaneCols<kF32> : kLaneCols<kBF16>;
     const bool aligned = dim % cols == 0 && out_stride % cols == 0 && weight_stride % cols == 0 && (uintptr_t)d_out_grad % 16 == 0 && (uintptr_t)d_weight_grad % (cols * we) == 0;
     if (n <= kFewTokens) {
-        // as many workgroups as keep the chip busy, and no more than that: each of them reads all token numbers
+        // as many workgroups as run side by side, four to a unit, and no more: each of them reads all token numbers (3000 tokens, 8000 bf16 rows of 200: 10.9 us,
+        // with twice as many 13.5)
         A.slices = (dim + 64 * cols - 1) / (64 * cols);
         A.rows = 4;
-        while (A.rows < kMaxFewRows && (vocab + A.rows - 1) / A.rows * A.slices > 2048) A.rows *= 2;
+        while (A.rows < kMaxFewRows && (vocab + A.rows - 1) / A.rows * A.slices > 1024) A.rows *= 2;
         const size_t groups = (vocab + A.rows - 1) / A.rows * A.slices;
         if (groups > kMostRows) return TCUSCAN_ERR_UNSUPPORTED;
         const void *fn = aligned ? pick<FewAligned>(out_dt, weight_dt) : pick<Few>(out_dt, weight_dt);
