@@ -786,13 +786,14 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(WalkArgs W)
     }
 }
 
-// out[t][stored head][i] = the sum of part[t][head][i] over the heads that share the stored head, in their order.  One pass, bound by reading fp32; four
-// elements a thread where the output allows stores of four (12289 tokens, 4 x 4 heads of 64: 9.4 us, one element a thread 15).
+// out[t][stored head][i] = the sum of part[t][head][i] over the heads that share the stored head, in their order, for the tokens that rows hold (others have
+// no part, and their outputs are not written).  One pass, bound by reading fp32; four elements a thread where the output allows stores of four (12289 tokens, 4 x 4 heads of 64: 9.4 us, one element a thread 15).
 struct SumArgs {
     const float *part;
     Heads out;
+    const long long *offsets;
     long long total;
-    unsigned heads, D;
+    unsigned rows, heads, D;
 };
 constexpr int kSumThreads = 256;
 template <int DT, int VEC> __global__ __launch_bounds__(kSumThreads) void sum_heads_kernel(SumArgs S)
@@ -803,7 +804,7 @@ template <int DT, int VEC> __global__ __launch_bounds__(kSumThreads) void sum_he
     const unsigned groups = S.D / VEC, each = groups * S.out.heads, group = S.heads / S.out.heads;          // (each: at most 2^24)
     const size_t i = (size_t)blockIdx.x * kSumThreads + threadIdx.x;
     const long long t = (long long)(i / each);
-    if (t >= S.total) return;
+    if (t >= S.total || t < S.offsets[0] || t >= S.offsets[S.rows]) return;
     const unsigned at = (unsigned)(i - (size_t)t * each), h = at / groups, d = (at - h * groups) * VEC;
     const float *p = S.part + ((size_t)t * S.heads + (size_t)h * group) * S.D + d;
     From sum = 0.0f;
@@ -1017,7 +1018,7 @@ tcuscan_status_t walk(WalkArgs W, Heads out, float *part, int dt, hipStream_t s,
     if (!shared || !W.total) return TCUSCAN_OK;
     const bool by_four = W.E % 4 == 0 && out.token % 4 == 0 && out.head % 4 == 0 && !misaligned(out.data, 4 * esz) && !misaligned(part, 16);
     const size_t blocks = ((size_t)W.total * out.heads * (W.E / (by_four ? 4 : 1)) + kSumThreads - 1) / kSumThreads;
-    SumArgs S = {part, out, W.total, W.heads, W.E};
+    SumArgs S = {part, out, W.offsets, W.total, W.rows, W.heads, W.E};
     if (blocks > kMostBlocks) return TCUSCAN_ERR_UNSUPPORTED;
     return launch(by_four ? pick<SumHeadsByFour>(dt) : pick<SumHeads>(dt), blocks, kSumThreads, &S, s) ? TCUSCAN_OK : TCUSCAN_ERR_HIP;
 }
