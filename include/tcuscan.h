@@ -378,6 +378,7 @@ tcuscan_status_t tcuscan_set_sort_fusion(int fused);
  *   d_ws       tcuscan_decay_attention_workspace_bytes(shape, dt, 0) bytes (its `backward` argument 1 for the gradients'), 16-byte
  *              aligned, zero-filled once.  An offset or slot out of range sets its fault word to 2
  *              (tcuscan_workspace_fault); nothing outside the arrays is touched then, and the results are unspecified.
+ *              A workspace serves every call with the same heads (in all and stored) and features, no more rows and no more tokens.
  *
  * Inputs must be finite.  A value that is not spoils outputs of its own row and heads, also up to 31 tokens in front of it, and none
  * of other rows.  What the products round on the way is far below the last bit of 16-bit outputs, and in fp32 about what fp32

@@ -933,29 +933,37 @@ tcuscan_status_t check_shape(const tcuscan_attention_shape_t *p, int dt)
 constexpr size_t kUnits = 256, kWantedGroups = 512;
 constexpr unsigned kWholeRows = 62;
 constexpr long long kMostUncutRow = 256, kMostUncut = 512;
+bool uncut(const tcuscan_attention_shape_t &s) { return s.total <= kMostUncut && s.total <= kMostUncutRow * s.rows; }
+size_t groups_of_a_token(const tcuscan_attention_shape_t &s) { return (size_t)s.heads * ((size_t)((s.dk > s.dv ? s.dk : s.dv) + 127) / 128); }
+size_t wanted_groups(const tcuscan_attention_shape_t &s) { return s.dk <= 64 && s.dv <= 64 && s.heads >= 8 ? 2 * kWantedGroups : kWantedGroups; }
 unsigned segment_log2_for(const tcuscan_attention_shape_t &s)
 {
-    if (s.total <= kMostUncut && s.total <= kMostUncutRow * s.rows) return kWholeRows;
-    const long long larger = s.dk > s.dv ? s.dk : s.dv;
-    const size_t work = (size_t)s.total * s.heads * ((size_t)(larger + 127) / 128), wanted = larger <= 64 && s.heads >= 8 ? 2 * kWantedGroups : kWantedGroups;
+    if (uncut(s)) return kWholeRows;
+    const size_t work = (size_t)s.total * groups_of_a_token(s);
     if (work >> 6 <= kUnits) return 6;
     unsigned log2 = 7;
-    while (work >> log2 > wanted) ++log2;
+    while (work >> log2 > wanted_groups(s)) ++log2;
     return (size_t)s.total >> log2 ? log2 : kWholeRows;
 }
 size_t pieces_for(const tcuscan_attention_shape_t &s, unsigned segment_log2) { return (size_t)s.rows + ((size_t)s.total >> segment_log2); }
+// The most segments beyond one a row that any call of up to s.total tokens makes: a call's segments double in length where they become too many, so it is not the
+// largest one that makes most.  (They hold at least 64 tokens, and their number times the groups of a token is at most what is wanted.)
+size_t most_segments(const tcuscan_attention_shape_t &s)
+{
+    const size_t shortest = (size_t)s.total >> 6, wanted = wanted_groups(s) / groups_of_a_token(s);
+    return uncut(s) ? 0 : shortest < wanted ? shortest : wanted;
+}
 
+// The workspace: the header, what lies between `pieces` segments (none: rows are not cut), parts of shared heads.
 struct Layout {
     size_t between, turned, part, all;
-    unsigned segment_log2;
-    Layout(const tcuscan_attention_shape_t &s, bool backward)
+    Layout(const tcuscan_attention_shape_t &s, bool backward, size_t pieces)
     {
-        segment_log2 = segment_log2_for(s);
         between = chain_layout::kHeaderBytes;
         turned = part = between;
-        if (segment_log2 != kWholeRows) {
+        if (pieces) {
             const size_t state = state_shape((unsigned)s.dk, (unsigned)s.dv).floats((unsigned)s.dv), other = state_shape((unsigned)s.dv, (unsigned)s.dk).floats((unsigned)s.dk);
-            const size_t all_states = pieces_for(s, segment_log2) * s.heads * 4;
+            const size_t all_states = pieces * s.heads * 4;
             turned = between + all_states * (backward && other > state ? other : state);
             part = turned + (backward ? all_states * other : 0);
         }
@@ -965,6 +973,19 @@ struct Layout {
             if (s.v_heads < s.heads && (size_t)s.dv > wide) wide = (size_t)s.dv;
         }
         all = part + (size_t)s.total * s.heads * wide * 4;
+    }
+};
+// How a call cuts its rows.  One that is cut although it has no more tokens than calls that are not may be given the workspace of such a call (512 tokens in two
+// rows, then in one): it is not cut then, either.
+struct Cut {
+    unsigned segment_log2;
+    size_t pieces;
+    Layout layout;
+    Cut(const tcuscan_attention_shape_t &s, bool backward, unsigned log2) : segment_log2(log2), pieces(pieces_for(s, log2)), layout(s, backward, log2 == kWholeRows ? 0 : pieces) {}
+    static Cut of(const tcuscan_attention_shape_t &s, bool backward, size_t ws_bytes)
+    {
+        const Cut wanted(s, backward, segment_log2_for(s));
+        return ws_bytes < wanted.layout.all && s.total <= kMostUncut ? Cut(s, backward, kWholeRows) : wanted;
     }
 };
 
@@ -1029,7 +1050,9 @@ extern "C" {
 
 size_t tcuscan_decay_attention_workspace_bytes(const tcuscan_attention_shape_t *shape, tcuscan_dtype_t dt, int backward)
 {
-    return check_shape(shape, dt) != TCUSCAN_OK ? 0 : Layout(*shape, backward != 0).all;
+    if (check_shape(shape, dt) != TCUSCAN_OK) return 0;
+    const size_t segments = most_segments(*shape);
+    return Layout(*shape, backward != 0, segments ? (size_t)shape->rows + segments : 0).all;
 }
 
 tcuscan_status_t tcuscan_decay_attention(const tcuscan_attention_shape_t *shape, const void *d_q, const void *d_k, const void *d_v, void *d_out,
@@ -1048,14 +1071,15 @@ tcuscan_status_t tcuscan_decay_attention(const tcuscan_attention_shape_t *shape,
         return TCUSCAN_ERR_INVALID_ARG;
     if (p.total && (d_out == d_q || d_out == d_k || d_out == d_v)) return TCUSCAN_ERR_INVALID_ARG;
     if (!d_slots && (d_state_in || d_state_out) && states < (size_t)p.rows) return TCUSCAN_ERR_INVALID_ARG;
-    const Layout L(p, false);
+    const Cut cut = Cut::of(p, false, ws_bytes);
+    const Layout &L = cut.layout;
     if (!d_ws || ws_bytes < L.all || misaligned(d_ws, 16)) return TCUSCAN_ERR_WORKSPACE;
     WalkArgs W = {};
     W.x = heads_of(d_q, p.q_token, p.q_head, p.q_heads);
     W.y = heads_of(d_k, p.k_token, p.k_head, p.k_heads);
     W.z = heads_of(d_v, p.v_token, p.v_head, p.v_heads);
     W.log_decay = d_log_decay; W.offsets = d_offsets; W.slots = d_slots; W.m_in = d_state_in; W.m_out = d_state_out; W.ws = d_ws;
-    W.between = (float *)((char *)d_ws + L.between); W.segment_log2 = L.segment_log2; W.pieces = (unsigned)pieces_for(p, L.segment_log2);
+    W.between = (float *)((char *)d_ws + L.between); W.segment_log2 = cut.segment_log2; W.pieces = (unsigned)cut.pieces;
     W.states = (long long)states; W.total = p.total; W.rows = (unsigned)p.rows; W.heads = (unsigned)p.heads;
     W.A = (unsigned)p.dk; W.E = (unsigned)p.dv; W.m_a = W.E; W.m_e = 1;
     W.by_new = 1.0f; W.by_read = scale; W.from_end = 0;
@@ -1086,7 +1110,8 @@ tcuscan_status_t tcuscan_decay_attention_backward(const tcuscan_attention_shape_
         if (d_q_grad == d_k_grad || d_q_grad == d_v_grad || d_k_grad == d_v_grad) return TCUSCAN_ERR_INVALID_ARG;
     }
     if (d_state_in_grad && (d_state_in_grad == d_state_in || d_state_in_grad == d_state_out_grad)) return TCUSCAN_ERR_INVALID_ARG;
-    const Layout L(p, true);
+    const Cut cut = Cut::of(p, true, ws_bytes);
+    const Layout &L = cut.layout;
     if (!d_ws || ws_bytes < L.all || misaligned(d_ws, 16)) return TCUSCAN_ERR_WORKSPACE;
     float *part = (float *)((char *)d_ws + L.part);
     hipStream_t s = (hipStream_t)stream;
@@ -1094,7 +1119,7 @@ tcuscan_status_t tcuscan_decay_attention_backward(const tcuscan_attention_shape_
                 v = heads_of(d_v, p.v_token, p.v_head, p.v_heads), o = heads_of(d_out_grad, p.o_token, p.o_head, p.heads);
     WalkArgs W = {};
     W.log_decay = d_log_decay; W.offsets = d_offsets; W.ws = d_ws;
-    W.between = (float *)((char *)d_ws + L.between); W.segment_log2 = L.segment_log2; W.pieces = (unsigned)pieces_for(p, L.segment_log2);
+    W.between = (float *)((char *)d_ws + L.between); W.segment_log2 = cut.segment_log2; W.pieces = (unsigned)cut.pieces;
     W.states = p.rows; W.total = p.total; W.rows = (unsigned)p.rows; W.heads = (unsigned)p.heads;
     const unsigned dk = (unsigned)p.dk, dv = (unsigned)p.dv;
     // dq, with the states of the forward pass: S^T
@@ -1105,7 +1130,7 @@ tcuscan_status_t tcuscan_decay_attention_backward(const tcuscan_attention_shape_
     // dv and the gradient by the first states, from the end: R
     W.by_new = scale; W.by_read = 1.0f; W.from_end = 1; W.m_in = d_state_out_grad; W.m_out = d_state_in_grad;
     W.x = k; W.y = q; W.z = o; W.A = dk; W.E = dv; W.m_a = dv; W.m_e = 1;
-    W.between_turned = L.segment_log2 != kWholeRows ? (float *)((char *)d_ws + L.turned) : nullptr;
+    W.between_turned = cut.segment_log2 != kWholeRows ? (float *)((char *)d_ws + L.turned) : nullptr;
     r = walk(W, heads_of(d_v_grad, p.dv_token, p.dv_head, p.v_heads), part, dt, s);
     if (r != TCUSCAN_OK) return r;
     // dk, with the same states, transposed: R^T.  What its segments start from is there.

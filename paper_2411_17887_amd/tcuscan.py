@@ -389,6 +389,7 @@ def new_decay_attention_workspace(rows: int, total: int, heads: int, d_k: int, d
 
 def new_decay_attention_backward_workspace(rows: int, total: int, heads: int, d_k: int, d_v: int, q_heads=None, k_heads=None, v_heads=None,
                                            dt="bf16"):
+    """The same for decay_attention_backward; q_heads, k_heads and v_heads where fewer are stored than `heads`."""
     return _zeros(decay_attention_workspace_bytes(rows, total, heads, d_k, d_v, q_heads, k_heads, v_heads, dt, backward=True))
 
 
