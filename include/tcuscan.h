@@ -162,7 +162,7 @@ tcuscan_status_t tcuscan_scan(const void *d_in, void *d_out, size_t rows, size_t
  * A segmented call of more than one launch keeps row maps in its workspace besides status words, at places that depend on
  * its shape, so it clears its status words in front of every run, and the library clears them again before another kind of call
  * uses the same workspace.  It cannot see a segmented call being REPLAYED from a graph: give such a graph a workspace that no
- * call outside the graph uses.
+ * call outside the graph uses.  (All this also goes for the workspaces of attention and of embedding gradients, below.)
  */
 size_t tcuscan_segmented_workspace_bytes(size_t rows, size_t total, tcuscan_dtype_t dt);
 tcuscan_status_t tcuscan_segmented(const void *d_in, void *d_out, const long long *d_offsets, size_t rows, size_t total,
@@ -208,7 +208,8 @@ tcuscan_status_t tcuscan_set_segmented_form(int flat);
  * `stream`.  1 means a carry-chain wait ran into its spin bound in some earlier
  * call (results of that call are invalid); this never happens in correct operation and
  * exists so that a protocol failure ends in an error instead of a hung GPU.  2 means a
- * segmented scan was given offsets that decrease or leave [0, total].
+ * segmented scan or an operator on tokens was given offsets that decrease or leave
+ * [0, total], or a slot or token number that is out of range.
  */
 tcuscan_status_t tcuscan_workspace_fault(const void *d_ws, tcuscan_stream_t stream, unsigned *h_fault);
 

@@ -24,6 +24,8 @@
 #include "element_types.h"
 #include "wave_ops.h"
 
+extern "C" void tcuscan_internal_workspace_reused(void *d_ws);                // tcuscan.hip
+
 namespace {
 
 constexpr int kMaxDim = 256;
@@ -1074,6 +1076,7 @@ tcuscan_status_t tcuscan_decay_attention(const tcuscan_attention_shape_t *shape,
     const Cut cut = Cut::of(p, false, ws_bytes);
     const Layout &L = cut.layout;
     if (!d_ws || ws_bytes < L.all || misaligned(d_ws, 16)) return TCUSCAN_ERR_WORKSPACE;
+    if (L.all > chain_layout::kHeaderBytes) tcuscan_internal_workspace_reused(d_ws);
     WalkArgs W = {};
     W.x = heads_of(d_q, p.q_token, p.q_head, p.q_heads);
     W.y = heads_of(d_k, p.k_token, p.k_head, p.k_heads);
@@ -1113,6 +1116,7 @@ tcuscan_status_t tcuscan_decay_attention_backward(const tcuscan_attention_shape_
     const Cut cut = Cut::of(p, true, ws_bytes);
     const Layout &L = cut.layout;
     if (!d_ws || ws_bytes < L.all || misaligned(d_ws, 16)) return TCUSCAN_ERR_WORKSPACE;
+    if (L.all > chain_layout::kHeaderBytes) tcuscan_internal_workspace_reused(d_ws);
     float *part = (float *)((char *)d_ws + L.part);
     hipStream_t s = (hipStream_t)stream;
     const Heads q = heads_of(d_q, p.q_token, p.q_head, p.q_heads), k = heads_of(d_k, p.k_token, p.k_head, p.k_heads),

@@ -16,6 +16,8 @@
 #include "element_types.h"
 #include "wave_ops.h"
 
+extern "C" void tcuscan_internal_workspace_reused(void *d_ws);                // tcuscan.hip
+
 namespace {
 
 constexpr int kThreads = 256;
@@ -511,6 +513,7 @@ tcuscan_status_t tcuscan_embedding_backward(const void *d_ids, int id_bytes, siz
         const void *fn = aligned ? pick<FewAligned>(out_dt, weight_dt) : pick<Few>(out_dt, weight_dt);
         return hipLaunchKernel(fn, dim3((unsigned)groups), dim3(64 * kWaves), args, 0, s) == hipSuccess ? TCUSCAN_OK : TCUSCAN_ERR_HIP;
     }
+    tcuscan_internal_workspace_reused(d_ws);       // (keys, tokens and sums, at places that depend on n; the sort's forms with a chain clear its status words)
     if (hipLaunchKernel((const void *)token_keys_kernel, dim3((unsigned)((n + kThreads - 1) / kThreads)), dim3(kThreads), args, 0, s) != hipSuccess) return TCUSCAN_ERR_HIP;
     int bits = 0;
     while (((size_t)1 << bits) <= vocab) ++bits;

@@ -3179,6 +3179,14 @@ tcuscan_status_t tcuscan_internal_split_pass(const void *d_keys, const void *d_v
     return hipLaunchKernel(fn, dim3(P.num_tiles), dim3(64 * W), args, 0, s) == hipSuccess ? TCUSCAN_OK : TCUSCAN_ERR_HIP;
 }
 
+// Used by the operators on tokens, which keep states, keys and sums in a workspace where a later call of another kind or size may expect status words: it is no
+// longer known to be clean.
+extern "C" __attribute__((visibility("hidden")))
+void tcuscan_internal_workspace_reused(void *d_ws)
+{
+    g_clean.mark_dirty((uintptr_t)d_ws, chain_tags::call_id(g_calls.load(std::memory_order_relaxed)).generation);
+}
+
 // Used by the sort (sort.hip): clearing, and the process-wide settings of the carry chain.
 extern "C" __attribute__((visibility("hidden")))
 hipError_t tcuscan_internal_fill(void *d, size_t bytes, hipStream_t s) { return launch_fill(d, bytes, s); }
