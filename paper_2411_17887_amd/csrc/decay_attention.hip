@@ -57,8 +57,11 @@ struct WalkArgs {
     int wide;                                      // the output is fp32 whatever the element type
 };
 
-// a^n, for weights.  (An n of 0 gives 1 for a decay of 0, a log_decay of minus infinity, too.)
-__device__ __forceinline__ float decay_power(float log_decay, float n) { return __expf(fmaxf(log_decay, -1e30f) * n); }
+// A log_decay of minus infinity as a number whose product with 0 is 0.  (Not by fmaxf, which would make a number of NaN: a model whose decays have gone wrong
+// gets NaN.)
+__device__ __forceinline__ float not_infinite(float log_decay) { return log_decay < -1e30f ? -1e30f : log_decay; }
+// a^n, for weights.  (An n of 0 gives 1 for a decay of 0, too.)
+__device__ __forceinline__ float decay_power(float log_decay, float n) { return __expf(not_infinite(log_decay) * n); }
 // Takes a state n tokens on: m becomes a^n m.  Slow decays (a^n from 1/2 on) as m + (a^n - 1) m: multiplied by a rounded a^n, a state
 // would be off by up to half a unit in the last place of 1 each time, always to the same side: 1e-5 for 1 - 2^-9 token by token.
 struct Decay {
@@ -66,7 +69,7 @@ struct Decay {
     bool slow;
     __device__ __forceinline__ Decay(float log_decay, float n)
     {
-        const float x = fmaxf(log_decay, -1e30f) * n;
+        const float x = not_infinite(log_decay) * n;
         slow = x > -0.69f;
         by = slow ? expm1f(x) : __expf(x);
     }
