@@ -381,6 +381,9 @@ tcuscan_status_t tcuscan_set_sort_fusion(int fused);
  *              (tcuscan_workspace_fault); nothing outside the arrays is touched then, and the results are unspecified.
  *              A workspace serves every call with the same heads (in all and stored) and features, no more rows and no more tokens.
  *
+ * Calls that would launch 2^32 threads or more (2^24 and more rows times heads times groups of 64 to 128 columns) are TCUSCAN_ERR_UNSUPPORTED; here and in the calls
+ * below nothing is enqueued then.
+ *
  * Inputs must be finite.  A value that is not spoils outputs of its own row and heads, also up to 31 tokens in front of it, and none
  * of other rows.  What the products round on the way is far below the last bit of 16-bit outputs, and in fp32 about what fp32
  * sums round.

@@ -909,8 +909,6 @@ template <int DT> struct SumHeadsByFour { static const void *fn() { return (cons
 template <int DT> struct Step { static const void *fn() { return (const void *)step_kernel<DT, 1>; } };
 template <int DT> struct StepByFour { static const void *fn() { return (const void *)step_kernel<DT, 4>; } };
 
-constexpr size_t kMostBlocks = 0x7FFFFFFFu;
-
 // What a call can do, by its sizes alone: TCUSCAN_OK, or why not.
 tcuscan_status_t check_shape(const tcuscan_attention_shape_t *p, int dt)
 {
@@ -922,7 +920,7 @@ tcuscan_status_t check_shape(const tcuscan_attention_shape_t *p, int dt)
         if (shared < 1 || shared > s.heads || s.heads % shared) return TCUSCAN_ERR_INVALID_ARG;
     if (s.dk > kMaxDim || s.dv > kMaxDim) return TCUSCAN_ERR_UNSUPPORTED;
     if (s.total >> 40) return TCUSCAN_ERR_UNSUPPORTED;
-    if (s.rows > 0x3FFFFFFF || s.heads > 0xFFFF || (unsigned long long)s.rows * s.heads > kMostBlocks / 8) return TCUSCAN_ERR_UNSUPPORTED;
+    if (s.rows > 0x3FFFFFFF || s.heads > 0xFFFF || (unsigned long long)s.rows * s.heads > 0xFFFFFFF) return TCUSCAN_ERR_UNSUPPORTED;
     return TCUSCAN_OK;
 }
 
@@ -1023,30 +1021,44 @@ bool whole(const Heads &x, unsigned dims, size_t esz)
            (x.token < 0 ? -x.token : x.token) < (1ll << 22);
 }
 
+// Gradients of heads that share `out`, added four columns a thread or one: threads, and how many columns.
+bool sums_by_four(const Heads &out, unsigned E, size_t esz)
+{
+    return E % 4 == 0 && out.token % 4 == 0 && out.head % 4 == 0 && !misaligned(out.data, 4 * esz);
+}
+size_t sum_groups(const Heads &out, long long total, unsigned E, size_t esz)
+{
+    return ((size_t)total * out.heads * (E / (sums_by_four(out, E, esz) ? 4 : 1)) + kSumThreads - 1) / kSumThreads;
+}
+size_t walk_groups(const WalkArgs &W, const StateShape &shape) { return (size_t)W.pieces * W.heads * ((W.E + shape.columns() - 1) / shape.columns()); }
+size_t join_groups(const WalkArgs &W, const StateShape &shape) { return (size_t)W.rows * W.heads * (shape.floats(W.E) / 4 / kJoinThreads); }
+// Whether a walk's launches can be made.
+bool launches_fit(const WalkArgs &W, const Heads &out, int dt)
+{
+    const StateShape shape = state_shape(W.A, W.E);
+    return walk_groups(W, shape) <= most_groups(64 * kWalkWaves) && (W.segment_log2 == kWholeRows || join_groups(W, shape) <= most_groups(kJoinThreads)) &&
+           (out.heads == W.heads || sum_groups(out, W.total, W.E, elem_bytes(dt)) <= most_groups(kSumThreads));
+}
+
 // One walk, into `out`; with heads that share the output, into `part` first.  `states_ready`: what the segments start from is in the workspace.
 tcuscan_status_t walk(WalkArgs W, Heads out, float *part, int dt, hipStream_t s, bool states_ready = false)
 {
     const size_t esz = elem_bytes(dt);
     const StateShape shape = state_shape(W.A, W.E);
-    const size_t groups = (size_t)W.pieces * W.heads * ((W.E + shape.columns() - 1) / shape.columns());
-    const size_t join_groups = (size_t)W.rows * W.heads * (shape.floats(W.E) / 4 / kJoinThreads);
-    if (groups > kMostBlocks || join_groups > kMostBlocks) return TCUSCAN_ERR_UNSUPPORTED;
+    const size_t groups = walk_groups(W, shape);
     const bool shared = out.heads < W.heads;
     const Heads to = shared ? Heads{part, (long long)W.heads * W.E, W.E, W.heads} : out;
     W.wide = shared;
     const bool new_whole = whole(W.y, W.A, esz) && whole(W.z, W.E, esz), all_whole = new_whole && whole(W.x, W.A, esz) && whole(to, W.E, shared ? 4 : esz) && to.token > 0;
     if (W.segment_log2 != kWholeRows && !states_ready) {
-        if (!launch(walk_for<false>(dt, W.A, new_whole, shape.CT), groups, 64 * kWalkWaves, &W, s) || !launch((const void *)join_kernel, join_groups, kJoinThreads, &W, s))
+        if (!launch(walk_for<false>(dt, W.A, new_whole, shape.CT), groups, 64 * kWalkWaves, &W, s) || !launch((const void *)join_kernel, join_groups(W, shape), kJoinThreads, &W, s))
             return TCUSCAN_ERR_HIP;
     }
     W.out = to;
     if (!launch(walk_for<true>(dt, W.A, all_whole, shape.CT), groups, 64 * kWalkWaves, &W, s)) return TCUSCAN_ERR_HIP;
     if (!shared || !W.total) return TCUSCAN_OK;
-    const bool by_four = W.E % 4 == 0 && out.token % 4 == 0 && out.head % 4 == 0 && !misaligned(out.data, 4 * esz) && !misaligned(part, 16);
-    const size_t blocks = ((size_t)W.total * out.heads * (W.E / (by_four ? 4 : 1)) + kSumThreads - 1) / kSumThreads;
     SumArgs S = {part, out, W.offsets, W.total, W.rows, W.heads, W.E};
-    if (blocks > kMostBlocks) return TCUSCAN_ERR_UNSUPPORTED;
-    return launch(by_four ? pick<SumHeadsByFour>(dt) : pick<SumHeads>(dt), blocks, kSumThreads, &S, s) ? TCUSCAN_OK : TCUSCAN_ERR_HIP;
+    return launch(sums_by_four(out, W.E, esz) ? pick<SumHeadsByFour>(dt) : pick<SumHeads>(dt), sum_groups(out, W.total, W.E, esz), kSumThreads, &S, s) ? TCUSCAN_OK : TCUSCAN_ERR_HIP;
 }
 
 }  // namespace
@@ -1079,7 +1091,6 @@ tcuscan_status_t tcuscan_decay_attention(const tcuscan_attention_shape_t *shape,
     const Cut cut = Cut::of(p, false, ws_bytes);
     const Layout &L = cut.layout;
     if (!d_ws || ws_bytes < L.all || misaligned(d_ws, 16)) return TCUSCAN_ERR_WORKSPACE;
-    if (L.all > chain_layout::kHeaderBytes) tcuscan_internal_workspace_reused(d_ws);
     WalkArgs W = {};
     W.x = heads_of(d_q, p.q_token, p.q_head, p.q_heads);
     W.y = heads_of(d_k, p.k_token, p.k_head, p.k_heads);
@@ -1089,7 +1100,10 @@ tcuscan_status_t tcuscan_decay_attention(const tcuscan_attention_shape_t *shape,
     W.states = (long long)states; W.total = p.total; W.rows = (unsigned)p.rows; W.heads = (unsigned)p.heads;
     W.A = (unsigned)p.dk; W.E = (unsigned)p.dv; W.m_a = W.E; W.m_e = 1;
     W.by_new = 1.0f; W.by_read = scale; W.from_end = 0;
-    return walk(W, heads_of(d_out, p.o_token, p.o_head, p.heads), nullptr, dt, (hipStream_t)stream);
+    const Heads out = heads_of(d_out, p.o_token, p.o_head, p.heads);
+    if (!launches_fit(W, out, dt)) return TCUSCAN_ERR_UNSUPPORTED;
+    if (L.all > chain_layout::kHeaderBytes) tcuscan_internal_workspace_reused(d_ws);
+    return walk(W, out, nullptr, dt, (hipStream_t)stream);
 }
 
 tcuscan_status_t tcuscan_decay_attention_backward(const tcuscan_attention_shape_t *shape, const void *d_q, const void *d_k, const void *d_v, const void *d_out_grad,
@@ -1119,32 +1133,38 @@ tcuscan_status_t tcuscan_decay_attention_backward(const tcuscan_attention_shape_
     const Cut cut = Cut::of(p, true, ws_bytes);
     const Layout &L = cut.layout;
     if (!d_ws || ws_bytes < L.all || misaligned(d_ws, 16)) return TCUSCAN_ERR_WORKSPACE;
-    if (L.all > chain_layout::kHeaderBytes) tcuscan_internal_workspace_reused(d_ws);
     float *part = (float *)((char *)d_ws + L.part);
     hipStream_t s = (hipStream_t)stream;
     const Heads q = heads_of(d_q, p.q_token, p.q_head, p.q_heads), k = heads_of(d_k, p.k_token, p.k_head, p.k_heads),
                 v = heads_of(d_v, p.v_token, p.v_head, p.v_heads), o = heads_of(d_out_grad, p.o_token, p.o_head, p.heads);
+    const Heads q_grad = heads_of(d_q_grad, p.dq_token, p.dq_head, p.q_heads), k_grad = heads_of(d_k_grad, p.dk_token, p.dk_head, p.k_heads),
+                v_grad = heads_of(d_v_grad, p.dv_token, p.dv_head, p.v_heads);
     WalkArgs W = {};
     W.log_decay = d_log_decay; W.offsets = d_offsets; W.ws = d_ws;
     W.between = (float *)((char *)d_ws + L.between); W.segment_log2 = cut.segment_log2; W.pieces = (unsigned)cut.pieces;
     W.states = p.rows; W.total = p.total; W.rows = (unsigned)p.rows; W.heads = (unsigned)p.heads;
     const unsigned dk = (unsigned)p.dk, dv = (unsigned)p.dv;
+    W.A = dk; W.E = dv;
+    if (!launches_fit(W, v_grad, dt)) return TCUSCAN_ERR_UNSUPPORTED;
+    W.A = dv; W.E = dk;
+    if (!launches_fit(W, q_grad, dt) || !launches_fit(W, k_grad, dt)) return TCUSCAN_ERR_UNSUPPORTED;
+    if (L.all > chain_layout::kHeaderBytes) tcuscan_internal_workspace_reused(d_ws);
     // dq, with the states of the forward pass: S^T
     W.x = o; W.y = v; W.z = k; W.A = dv; W.E = dk; W.m_a = 1; W.m_e = dv; W.m_in = d_state_in;
     W.by_new = 1.0f; W.by_read = scale; W.from_end = 0;
-    tcuscan_status_t r = walk(W, heads_of(d_q_grad, p.dq_token, p.dq_head, p.q_heads), part, dt, s);
+    tcuscan_status_t r = walk(W, q_grad, part, dt, s);
     if (r != TCUSCAN_OK) return r;
     // dv and the gradient by the first states, from the end: R
     W.by_new = scale; W.by_read = 1.0f; W.from_end = 1; W.m_in = d_state_out_grad; W.m_out = d_state_in_grad;
     W.x = k; W.y = q; W.z = o; W.A = dk; W.E = dv; W.m_a = dv; W.m_e = 1;
     W.between_turned = cut.segment_log2 != kWholeRows ? (float *)((char *)d_ws + L.turned) : nullptr;
-    r = walk(W, heads_of(d_v_grad, p.dv_token, p.dv_head, p.v_heads), part, dt, s);
+    r = walk(W, v_grad, part, dt, s);
     if (r != TCUSCAN_OK) return r;
     // dk, with the same states, transposed: R^T.  What its segments start from is there.
     W.m_out = nullptr;
     W.between = W.between_turned;
     W.x = v; W.y = o; W.z = q; W.A = dv; W.E = dk; W.m_a = 1; W.m_e = dv;
-    return walk(W, heads_of(d_k_grad, p.dk_token, p.dk_head, p.k_heads), part, dt, s, true);
+    return walk(W, k_grad, part, dt, s, true);
 }
 
 tcuscan_status_t tcuscan_decay_attention_step(const tcuscan_attention_shape_t *shape, const void *d_q, const void *d_k, const void *d_v, void *d_out,
@@ -1173,7 +1193,7 @@ tcuscan_status_t tcuscan_decay_attention_step(const tcuscan_attention_shape_t *s
     while ((1u << S.lanes_log2) < row_lanes && S.lanes_log2 < 6) ++S.lanes_log2;
     while (S.lanes_log2 > 3 && all * ((row_lanes + (1u << S.lanes_log2) - 1) >> S.lanes_log2) < kWantedGroups) --S.lanes_log2;
     S.blocks = (row_lanes + (1u << S.lanes_log2) - 1) >> S.lanes_log2;
-    if (all * S.blocks > kMostBlocks) return TCUSCAN_ERR_UNSUPPORTED;
+    if (all * S.blocks > most_groups(kStepThreads)) return TCUSCAN_ERR_UNSUPPORTED;
     return launch(vec == 4 ? pick<StepByFour>(dt) : pick<Step>(dt), all * S.blocks, kStepThreads, &S, (hipStream_t)stream) ? TCUSCAN_OK : TCUSCAN_ERR_HIP;
 }
 

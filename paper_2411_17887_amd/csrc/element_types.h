@@ -21,6 +21,9 @@ template <> struct Elem<kBF16> { typedef bf16_t T; };
 
 inline size_t elem_bytes(int dt) { return dt == kF32 ? 4 : dt == kF16 || dt == kBF16 ? 2 : 0; }
 
+// Workgroups of `threads` that one launch holds: HIP takes fewer than 2^32 threads.  Calls beyond it are refused before anything is enqueued.
+constexpr size_t most_groups(size_t threads) { return 0xFFFFFFFFu / threads; }
+
 // Raised where a device array holds an offset, slot or token number that is out of range (chain_layout.h: the header's first word).
 constexpr uint32_t kFaultBadIndex = 2u;
 __device__ __forceinline__ void raise_fault(void *ws, uint32_t fault)

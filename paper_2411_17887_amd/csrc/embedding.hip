@@ -465,7 +465,7 @@ tcuscan_status_t tcuscan_embedding(const void *d_ids, int id_bytes, size_t n, co
     const bool aligned = dim % cols == 0 && weight_stride % cols == 0 && out_stride % cols == 0 && (uintptr_t)d_weight % 16 == 0 && (uintptr_t)d_out % 16 == 0;
     const bool many = n * slices >= kManyItems;
     const size_t at_once = many ? kTokensAtOnce : 1, blocks = ((n + at_once - 1) / at_once * slices + kThreads / 64 - 1) / (kThreads / 64);
-    if (blocks > kMostRows) return TCUSCAN_ERR_UNSUPPORTED;
+    if (blocks > most_groups(kThreads)) return TCUSCAN_ERR_UNSUPPORTED;
     LookupArgs A = {d_ids, d_weight, d_out, d_ws, n, vocab, dim, weight_stride, out_stride, slices, scale, id_bytes == 8};
     void *args[] = {&A};
     const void *fn = many ? aligned ? pick<LookupManyAligned>(weight_dt, out_dt) : pick<LookupMany>(weight_dt, out_dt)
@@ -509,26 +509,25 @@ tcuscan_status_t tcuscan_embedding_backward(const void *d_ids, int id_bytes, siz
         A.rows = 4;
         while (A.rows < kMaxFewRows && (vocab + A.rows - 1) / A.rows * A.slices > 1024) A.rows *= 2;
         const size_t groups = (vocab + A.rows - 1) / A.rows * A.slices;
-        if (groups > kMostRows) return TCUSCAN_ERR_UNSUPPORTED;
+        if (groups > most_groups(64 * kWaves)) return TCUSCAN_ERR_UNSUPPORTED;
         const void *fn = aligned ? pick<FewAligned>(out_dt, weight_dt) : pick<Few>(out_dt, weight_dt);
         return hipLaunchKernel(fn, dim3((unsigned)groups), dim3(64 * kWaves), args, 0, s) == hipSuccess ? TCUSCAN_OK : TCUSCAN_ERR_HIP;
     }
+    A.slices = (dim + 64 * cols - 1) / (64 * cols);
+    const size_t pieces = (n + kPiece - 1) / kPiece, zero_groups = accumulate ? 0 : (vocab + kZeroRows - 1) / kZeroRows;
+    A.zero_groups = zero_groups;
+    A.piece_groups = (pieces * A.slices + kThreads / 64 - 1) / (kThreads / 64);
+    const size_t by = aligned ? 4 : 1, join_groups = pieces * ((dim + 64 * by - 1) / (64 * by)), key_groups = (n + kThreads - 1) / kThreads;
+    if (key_groups > most_groups(kThreads) || A.piece_groups + zero_groups > most_groups(kThreads) || join_groups > most_groups(64 * kJoinWaves)) return TCUSCAN_ERR_UNSUPPORTED;
     tcuscan_internal_workspace_reused(d_ws);       // (keys, tokens and sums, at places that depend on n; the sort's forms with a chain clear its status words)
-    if (hipLaunchKernel((const void *)token_keys_kernel, dim3((unsigned)((n + kThreads - 1) / kThreads)), dim3(kThreads), args, 0, s) != hipSuccess) return TCUSCAN_ERR_HIP;
+    if (hipLaunchKernel((const void *)token_keys_kernel, dim3((unsigned)key_groups), dim3(kThreads), args, 0, s) != hipSuccess) return TCUSCAN_ERR_HIP;
     int bits = 0;
     while (((size_t)1 << bits) <= vocab) ++bits;
     const tcuscan_status_t st = tcuscan_split_radix_sort_u32(A.keys, A.tokens, n, bits, ws + L.keys_tmp, ws + L.tokens_tmp, ws + L.flags, ws + L.positions,
                                                              d_ws, L.chain, stream);
     if (st != TCUSCAN_OK) return st;
-    A.slices = (dim + 64 * cols - 1) / (64 * cols);
-    const size_t pieces = (n + kPiece - 1) / kPiece, zero_groups = accumulate ? 0 : (vocab + kZeroRows - 1) / kZeroRows;
-    A.zero_groups = zero_groups;
-    A.piece_groups = (pieces * A.slices + kThreads / 64 - 1) / (kThreads / 64);
-    if (A.piece_groups + zero_groups > kMostRows) return TCUSCAN_ERR_UNSUPPORTED;
     const void *fn = aligned ? pick<RunsAligned>(out_dt, weight_dt) : pick<Runs>(out_dt, weight_dt);
     if (hipLaunchKernel(fn, dim3((unsigned)(A.piece_groups + zero_groups)), dim3(kThreads), args, 0, s) != hipSuccess) return TCUSCAN_ERR_HIP;
-    const size_t by = aligned ? 4 : 1, join_groups = pieces * ((dim + 64 * by - 1) / (64 * by));
-    if (join_groups > kMostRows) return TCUSCAN_ERR_UNSUPPORTED;
     fn = weight_dt == kF16 ? aligned ? (const void *)join_runs_kernel<kF16, 4> : (const void *)join_runs_kernel<kF16, 1>
        : weight_dt == kF32 ? aligned ? (const void *)join_runs_kernel<kF32, 4> : (const void *)join_runs_kernel<kF32, 1>
                            : aligned ? (const void *)join_runs_kernel<kBF16, 4> : (const void *)join_runs_kernel<kBF16, 1>;
