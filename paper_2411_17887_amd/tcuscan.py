@@ -450,7 +450,7 @@ def decay_attention_step(q, k, v, out, log_decay, state, slots=None, scale: floa
 
 def _check_tokens(ids, rows, table) -> None:
     """ids: n dense integers of 4 or 8 bytes; rows [n, dim] and table [vocab, dim] with dense features."""
-    _refuse(ids.dtype.is_floating_point or ids.element_size() not in (4, 8) or not ids.is_contiguous(), "ids: a dense tensor of 4- or 8-byte integers is wanted")
+    _refuse(ids.dtype.is_floating_point or ids.dtype.is_complex or ids.element_size() not in (4, 8) or not ids.is_contiguous(), "ids: a dense tensor of 4- or 8-byte integers is wanted")
     _refuse(rows.dim() != 2 or table.dim() != 2 or rows.shape[0] != ids.numel() or rows.shape[1] != table.shape[1], "one row of the table's width per token is wanted")
     _refuse((rows.stride(1) != 1 or table.stride(1) != 1) and table.shape[1] > 1, "features have to be dense")
 
