@@ -828,7 +828,7 @@ struct StepArgs {
     float *state;
     void *ws;
     long long states;
-    unsigned n, heads, A, E, blocks, lanes_log2;
+    unsigned heads, A, E, blocks, lanes_log2;
     float scale;
 };
 constexpr int kStepThreads = 256;
@@ -1186,7 +1186,7 @@ tcuscan_status_t tcuscan_decay_attention_step(const tcuscan_attention_shape_t *s
     S.q = heads_of(d_q, p.q_token, p.q_head, p.q_heads); S.k = heads_of(d_k, p.k_token, p.k_head, p.k_heads);
     S.v = heads_of(d_v, p.v_token, p.v_head, p.v_heads); S.out = heads_of(d_out, p.o_token, p.o_head, p.heads);
     S.log_decay = d_log_decay; S.slots = d_slots; S.state = d_state; S.ws = d_ws; S.states = (long long)states;
-    S.n = (unsigned)p.rows; S.heads = (unsigned)p.heads; S.A = (unsigned)p.dk; S.E = (unsigned)p.dv; S.scale = scale;
+    S.heads = (unsigned)p.heads; S.A = (unsigned)p.dk; S.E = (unsigned)p.dv; S.scale = scale;
     // lanes to a row: all of it, up to a wavefront; 128 bytes where there are few states, for more workgroups
     const unsigned vec = S.E % 4 == 0 ? 4 : 1, row_lanes = (S.E + vec - 1) / vec;
     const size_t all = (size_t)p.rows * p.heads;
