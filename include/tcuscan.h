@@ -385,8 +385,9 @@ tcuscan_status_t tcuscan_set_sort_fusion(int fused);
  * below nothing is enqueued then.
  *
  * Inputs must be finite.  A value that is not spoils outputs of its own row and heads, also up to 31 tokens in front of it, and none
- * of other rows.  What the products round on the way is far below the last bit of 16-bit outputs, and in fp32 about what fp32
- * sums round.
+ * of other rows.  A log_decay that is not a number makes its head's outputs and states so.  What is rounded on the way to an output
+ * goes by the sizes of its terms, not by their sum: at most 2^-15 of the sum of their absolute values for bf16 and 2^-14 for f16, which
+ * shows only where terms cancel; fp32, and states whatever the type, about what fp32 sums round.
  */
 typedef struct {
     long long rows, total, heads, dk, dv;
