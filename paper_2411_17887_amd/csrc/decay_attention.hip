@@ -125,10 +125,12 @@ __device__ __forceinline__ long long state_of(const long long *slots, unsigned r
 // read transposed once, for Z^T P^T and, weighted, for the update.  Only X, Y and Z, which all wavefronts of a workgroup share, go through LDS.
 //
 // What it costs.  A row of many tokens is cut into segments, so Y and Z are read twice: once for what each segment adds to the state, then, with what
-// each segment starts from (join_kernel), for the outputs.  65536 bf16 tokens, 16 heads of 128 x 128 (inputs and outputs 1.08 GB, 1.61 GB moved): 117 us for the
-// first reading (4.6 TB/s, a large copy's rate), 14 for the join, 250 for the outputs (4.3 TB/s); with all inputs in L2 77 and 195.  Memory bounds it, then
-// the matrix unit, which is busy a third of the time.  f16 and fp32 multiply three and six pairs of parts and are bound by the matrix unit and by splitting:
-// 20011 f16 tokens, 16 heads of 80 x 96, 81 + 10 + 158 us.  In short rows the time is that of blocks in a row, 2 us each.
+// each segment starts from (join_kernel), for the outputs.  65536 bf16 tokens, 16 heads of 128 x 128 (inputs and outputs 1.08 GB, 1.73 GB moved): 117 us for the
+// first reading (0.55 GB, 4.7 TB/s where streaming reaches 6.5), 14 for the join, 247 for the outputs (1.1 GB, 4.5 TB/s); with all inputs in L2 78 and 211.  So
+// the walk itself is most of it: vector instructions (half of the outputs' cycles, the scores among them, which each of the four wavefronts computes for itself)
+// and the matrix unit (busy a third of them), in the order in which one block's products wait for each other.  f16 and fp32 multiply three and six pairs of parts and
+// split their inputs on the way: 20011 f16 tokens in 30 ragged rows, 16 heads of 80 x 96, 80 + 9 + 160 us; the units work 60 % of the last and wait for the
+// longest rows' ends.  In short rows the time is that of blocks in a row, 2 us each.
 //
 // Precision.  The matrix unit multiplies bf16 and adds in fp32, so every operand is a sum of bf16 parts: bf16 inputs one, f16 two (exact),
 // fp32 three.  What is rounded on the way:
@@ -793,7 +795,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(WalkArgs W)
 }
 
 // out[t][stored head][i] = the sum of part[t][head][i] over the heads that share the stored head, in their order, for the tokens that rows hold (others have
-// no part, and their outputs are not written).  One pass, bound by reading fp32; four elements a thread where the output allows stores of four (12289 tokens, 4 x 4 heads of 64: 9.4 us, one element a thread 15).
+// no part, and their outputs are not written).  One pass, bound by reading fp32; four elements a thread where the output allows stores of four (12289 tokens, 4 x 4 heads of 64: 10 us, one element a thread 15).
 struct SumArgs {
     const float *part;
     Heads out;
@@ -820,7 +822,7 @@ template <int DT, int VEC> __global__ __launch_bounds__(kSumThreads) void sum_he
 
 // One token for each of many sequences.  A workgroup takes a block of columns of one state: 2^lanes_log2 lanes to a row, VEC columns each, as many rows at
 // a time as the workgroup has lanes for; the state stays in registers between its product with q and its writing.  The state is read and written once and
-// nothing else counts: 256 sequences of 16 heads of 128 x 128 (537 MB) take 112 us, 4.8 TB/s, a large copy's rate; one sequence, whose columns are spread over
+// nothing else counts: 256 sequences of 16 heads of 128 x 128 (537 MB) take 112 us, 4.8 TB/s (streaming from one array to another 6.5); one sequence, whose columns are spread over
 // as many workgroups as there are columns for, the time of a launch.
 struct StepArgs {
     Heads q, k, v, out;

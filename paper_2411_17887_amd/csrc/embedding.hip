@@ -96,8 +96,8 @@ template <int DG, int DOTHER, bool ALIGNED> struct Lane {
 };
 
 // A wavefront takes a slice of the columns of kTokens tokens: their loads are on their way together.  (kTokens = 1: few tokens, whose columns are spread
-// over as many wavefronts as there are.)  Bound by memory: 65536 bf16 rows of 1024 from an fp32 table (74 MB of it read, 134 MB written) take 43 us,
-// 4.8 TB/s; 24 rows of 2048 2.5 us, their loads one after the other: the number, the row.
+// over as many wavefronts as there are.)  Bound by memory: 65536 bf16 rows of 1024 from an fp32 table (74 MB of it read, 134 MB written) take 44 us,
+// 4.7 TB/s (streaming reaches 6.1 to 6.5); 24 rows of 2048 2.5 us, their loads one after the other: the number, the row.
 template <int DW, int DO, bool ALIGNED, int kTokens> __global__ __launch_bounds__(kThreads) void lookup_kernel(LookupArgs A)
 {
     typedef Lane<DW == kF32 ? DO : DW, DW == kF32 ? DW : DO, ALIGNED> L;       // (eight columns to a lane unless both types are fp32)
@@ -273,7 +273,7 @@ template <int DG, int DW, bool ALIGNED> __global__ __launch_bounds__(64 * kWaves
 // wavefronts: a wavefront takes a piece and a slice of the columns.  Runs that lie inside a piece are finished there; what a piece has of
 // a run that goes on beyond it is kept, in fp32, in one of the piece's two places (0: the run comes from the piece before, 1: it starts here)
 // and added up, piece by piece in their order, by join_runs_kernel.  Every second workgroup, as long as both are left, writes zeros into rows that no token took.
-// Bound by memory: 65536 bf16 gradients of 1024 columns into 65536 fp32 rows (134 MB read, 268 written) take 97 us, 4.2 TB/s, after a sort of 35.
+// Bound by memory: 65536 bf16 gradients of 1024 columns into 65536 fp32 rows (134 MB read, 268 written) take 95 us, 4.2 TB/s, after a sort of 35.
 constexpr int kPiece = 32, kZeroRows = 64;
 template <int DG, int DW, bool ALIGNED> __global__ __launch_bounds__(kThreads) void sum_runs_kernel(GradArgs A)
 {
@@ -503,8 +503,8 @@ tcuscan_status_t tcuscan_embedding_backward(const void *d_ids, int id_bytes, siz
     const size_t cols = out_dt == kF32 ? kLaneCols<kF32> : kLaneCols<kBF16>;
     const bool aligned = dim % cols == 0 && out_stride % cols == 0 && weight_stride % cols == 0 && (uintptr_t)d_out_grad % 16 == 0 && (uintptr_t)d_weight_grad % (cols * we) == 0;
     if (n <= kFewTokens) {
-        // as many workgroups as run side by side, four to a unit, and no more: each of them reads all token numbers (3000 tokens, 8000 bf16 rows of 200: 10.9 us,
-        // with twice as many 13.5)
+        // up to 1024 workgroups, as many as run side by side for fp32 gradients (43 to 46 registers: four to a unit; three for 16-bit ones, which take 74 to 77), and
+        // no more: each of them reads all token numbers (3000 tokens, 8000 bf16 rows of 200: 10.9 us, with twice as many 13.5)
         A.slices = (dim + 64 * cols - 1) / (64 * cols);
         A.rows = 4;
         while (A.rows < kMaxFewRows && (vocab + A.rows - 1) / A.rows * A.slices > 1024) A.rows *= 2;
