@@ -134,7 +134,7 @@ __device__ __forceinline__ long long state_of(const long long *slots, unsigned r
 //
 // Precision.  The matrix unit multiplies bf16 and adds in fp32, so every operand is a sum of bf16 parts: bf16 inputs one, f16 two (exact),
 // fp32 three.  What is rounded on the way:
-//   * what is added to a state, by_new a^(C-1-j) z_j: three parts (24 bits) where the row's last state is asked for and this much of it is left there, so that
+//   * what is added to a state, by_new a^(C-1-j) z_j: three parts (24 bits) where the row's last state is asked for and any of it is left there, so that
 //     states come out as exact as fp32 sums make them; two (16 bits) where only 16-bit outputs are read from it
 //   * the state, where it is read: two parts (16 bits), three for fp32
 //   * the weighted scores P: two parts, three for fp32 (one part would do for bf16 but for its error, as large as that of the rounded output: 0.0024 of the
@@ -535,10 +535,11 @@ template <int DT, int AP, int CT, bool WHOLE, bool READS> __global__ __launch_bo
     char *out = (char *)W.out.data + (W.out.at(h, W.heads) + origin * W.out.token) * out_size + (sign < 0 ? 15 * out_step : 0);
     typedef std::conditional_t<WHOLE, unsigned, long long> Offset;
     const Offset out_lane = (Offset)((sign < 0 ? l - 15 : l) * out_step) + (Offset)(col * out_size);         // (not negative: outputs have positive strides)
-    // The third part of what is added to a state counts where the state itself is asked for, not where 16-bit outputs are read from it; and there for the tokens
-    // of which more than an eighth is left at the end of the row (the two parts are 3e-6 off: less than the last bits of fp32 sums then).
+    // The third part of what is added to a state counts where the state itself is asked for, not where 16-bit outputs are read from it; and there for the segments
+    // of which more than 2^-24 is left at the end of the row (beyond, two parts are off by 2^-40 of what was added.  With the limit at 1/8 65536 tokens take 380 us,
+    // with this one 387, without one 405; but a state to which the last tokens add little would have 16 bits where fp32 sums have 24).
     constexpr int kParts = N == 3 ? 3 : 2;
-    const bool exact = W.m_out && slot >= 0 && decay_power(log_decay, (float)(piece.hi - piece.lo - piece.end)) > 0.125f;
+    const bool exact = W.m_out && slot >= 0 && decay_power(log_decay, (float)(piece.hi - piece.lo - piece.end)) > 0x1p-24f;
     const long long length = piece.end - piece.first;
     auto tokens = [&](long long left) { return (int)(left < C ? left : C); };
     // by_new a^(n-1-j), from the end a^(n-j), of the lane's tokens j = column_row(g, k): in whole blocks a power for the lane's group times one for k, which is
