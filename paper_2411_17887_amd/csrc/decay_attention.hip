@@ -125,11 +125,11 @@ __device__ __forceinline__ long long state_of(const long long *slots, unsigned r
 // read transposed once, for Z^T P^T and, weighted, for the update.  Only X, Y and Z, which all wavefronts of a workgroup share, go through LDS.
 //
 // What it costs.  A row of many tokens is cut into segments, so Y and Z are read twice: once for what each segment adds to the state, then, with what
-// each segment starts from (join_kernel), for the outputs.  65536 bf16 tokens, 16 heads of 128 x 128 (inputs and outputs 1.08 GB, 1.73 GB moved): 117 us for the
-// first reading (0.55 GB, 4.7 TB/s where streaming reaches 6.5), 14 for the join, 247 for the outputs (1.1 GB, 4.5 TB/s); with all inputs in L2 78 and 211.  So
+// each segment starts from (join_kernel), for the outputs.  65536 bf16 tokens, 16 heads of 128 x 128 (inputs and outputs 1.08 GB, 1.73 GB moved): 125 us for the
+// first reading (0.55 GB, 4.4 TB/s where streaming reaches 6.5), 14 for the join, 250 for the outputs (1.1 GB, 4.4 TB/s); with all inputs in L2 97 and 206.  So
 // the walk itself is most of it: vector instructions (half of the outputs' cycles, the scores among them, which each of the four wavefronts computes for itself)
 // and the matrix unit (busy a third of them), in the order in which one block's products wait for each other.  f16 and fp32 multiply three and six pairs of parts and
-// split their inputs on the way: 20011 f16 tokens in 30 ragged rows, 16 heads of 80 x 96, 80 + 9 + 160 us; the units work 60 % of the last and wait for the
+// split their inputs on the way: 20011 f16 tokens in 30 ragged rows, 16 heads of 80 x 96, 81 + 9 + 162 us; the units work 60 % of the last and wait for the
 // longest rows' ends.  In short rows the time is that of blocks in a row, 2 us each.
 //
 // Precision.  The matrix unit multiplies bf16 and adds in fp32, so every operand is a sum of bf16 parts: bf16 inputs one, f16 two (exact),
